@@ -110,13 +110,14 @@ def _spread(n, lo, hi, g, dev):
 
 
 def _table(lens, page, g, dev):
-    """Block tables of requests that hold lens[b] tokens: pages in a random order, -1 past the last."""
+    """Block tables of requests that hold lens[b] tokens: pages in a random order, -1 past the last; and the pool's
+    pages, as many as so many tokens of so many requests can take."""
     used = (lens.long() + page - 1) // page
-    W, total = int(used.max()), int(used.sum())
-    ids = torch.randperm(total + 3, device=dev, generator=g)
+    W, pool = int(used.max()), (int(lens.sum()) + lens.numel() * (page - 1)) // page + 3
+    ids = torch.randperm(pool, device=dev, generator=g)
     col = torch.arange(W, device=dev)[None]
     at = (used.cumsum(0) - used)[:, None] + col
-    return torch.where(col < used[:, None], ids[at.clamp(max=total - 1)], -1).to(torch.int32), total + 3
+    return torch.where(col < used[:, None], ids[at.clamp(max=pool - 1)], -1).to(torch.int32), pool
 
 
 def _cache(c, pages, width, g, dev):
@@ -233,7 +234,7 @@ def _map(s):
     tokens = added.clamp(min=0)
     end = tokens.cumsum(0)
     taken = need.cumsum(0)
-    served = valid & (end <= N) & ((need == 0) | (taken <= free.numel()))
+    served = valid & ((tokens == 0) | (end <= N)) & ((need == 0) | (taken <= free.numel()))
     col = torch.arange(W, device=free.device)[None]
     fresh = served[:, None] & (col >= have[:, None]) & (col < want[:, None])
     src = (taken - need)[:, None] + col - have[:, None]
