@@ -426,6 +426,134 @@ rel_status relation_linear_gated_bwd(const rel_problem* p, const void* p1, const
                                      float* da_log, float* ddt_bias, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Serving from a paged cache. Keys and values live in a pool of pages of
+ * page_size tokens; a request's block table names its pages in order. A step
+ * of a serving loop is: relation_page_map (pages and slots of the step's
+ * tokens), relation_paged_append (their rows into the pages),
+ * relation_paged_decode (one new row per request and head), and, on the
+ * model's logits, relation_sample. Lengths, page ids, slots and sampling
+ * parameters are device data that the host cannot check; the kernels read and
+ * write only inside the buffers described here whatever they hold.
+ *
+ * rel_pages describes the two pools (keys and values share it): row (page,
+ * head, offset) of D elements at page * stride_page + head * stride_head +
+ * offset * stride_token, the elements of a row contiguous. Both [pages, H,
+ * page_size, D] and [pages, page_size, H, D] are such layouts, and the two
+ * pools may be interleaved in one allocation. */
+typedef struct rel_pages {
+  int64_t num_pages;  /* at most 2^28 */
+  int64_t page_size;  /* tokens per page: a power of two, 1 to 65536 */
+  int64_t H;          /* key/value heads, at most 2^16 */
+  int64_t D;          /* row width: a multiple of 16 bytes, at most 128 elements */
+  int32_t dtype;      /* rel_dtype of the pools, q, k, v and out */
+  int64_t stride_page, stride_head, stride_token; /* elements, multiples of 16 bytes; a page spans < 2^31 elements */
+} rel_pages;
+
+/* Block tables and slots of a step, from lengths. Request b holds cached[b]
+ * tokens, in the first ceil(cached[b] / page_size) pages of its table row, and
+ * adds added[b] (0 for one that waits). With have and want the pages for
+ * cached[b] and cached[b] + added[b] tokens, it takes want - have pages from
+ * free_pages, in the order of the list, requests in their order.
+ *   table      in/out int32 [B, table_width]: entries have .. want - 1 of each
+ *              served request are written, no others
+ *   lengths    out int32 [B]: cached[b] + added[b]; 0 if not served
+ *   row_start  out int32 [B + 1]: where the request's tokens stand among the
+ *              step's, packed in the requests' order (sums of added[b], a
+ *              negative one as 0), at most max_tokens
+ *   slots      out int64 [max_tokens]: page * page_size + offset of each token;
+ *   positions  out int32 [max_tokens]: its position, from cached[b] on. Both
+ *              -1 past the last token and for requests not served
+ *   counts     out int32 [3]: pages taken (always the first of free_pages),
+ *              tokens mapped, requests not served
+ * A request is not served (nothing of it is written but the values above) if a
+ * count is negative, the table row is too short for it, its tokens pass
+ * max_tokens, or it needs pages and the list is used up by those before it
+ * (needs of requests that are short count as well, so none that needs pages is
+ * served after one that found too few). page_size as in rel_pages; B at most
+ * 4096, the other sizes 2^30. One launch, no workspace. */
+typedef struct rel_page_map {
+  int64_t B, table_width, page_size, max_tokens, num_free;
+} rel_page_map;
+rel_status relation_page_map(const rel_page_map* m, const int32_t* cached, const int32_t* added,
+                             const int32_t* free_pages, int32_t* table, int32_t* lengths, int32_t* row_start,
+                             int64_t* slots, int32_t* positions, int32_t* counts, void* stream);
+
+/* The rows of new tokens into the cache: RoPE on q and k at the tokens'
+ * positions, Givens mixing of v (Sec. 3.1, eq. 4; as relation_layer_fwd does
+ * them), zeros in channels D .. c->D - 1.
+ *   q          [N, Hq, D], optional: the new queries   k, v  [N, H, D], H = c->H
+ *              (element strides below, rows contiguous, any alignment of the
+ *              element; 16-byte rows are fastest)
+ *   slots      int64 [N]; positions int32 [N]. A token with a negative slot or
+ *              position, or a slot past the pool, is not written and its q_out
+ *              row is 0. Two tokens with one slot: either's row remains.
+ *   theta      fp32 [H/2] Givens angles (givens != NONE, H even)
+ *   q_out      [N, Hq, c->D], dense, 16-byte aligned: rotated and padded
+ *              queries, as relation_paged_decode takes them (with q)
+ *   k_cache, v_cache  the pools, described by c. Rows of no token keep their values.
+ * Angles are formed in 64 bits; sums in fp32, rounded once to the dtype. */
+typedef struct rel_append {
+  int64_t N, Hq, D;                 /* tokens, query heads, true head width (even with RoPE) */
+  int64_t q_token, q_head;          /* strides of q */
+  int64_t kv_token, kv_head;        /* strides shared by k and v */
+  double rope_base;                 /* 0: no RoPE; else > 1 */
+  int32_t givens;                   /* rel_givens */
+} rel_append;
+rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const void* q, const void* k, const void* v,
+                                 const int64_t* slots, const int32_t* positions, const float* theta, void* q_out,
+                                 void* k_cache, void* v_cache, void* stream);
+
+/* Decode step over pages: relation_decode with the cache in pages, and query
+ * heads that may share key heads (query head h reads key head h / (Hq / H)).
+ * The new token's rows must be in the cache already, as entry lengths[b].
+ *   q          [B, Hq, D] dense, 16-byte aligned   out  the same
+ *   table      int32 [B, table_width]; lengths int32 [B]
+ *   row_stat   fp32 [B, Hq], optional: M_i = ln Z_i + lambda ln i
+ *   workspace  relation_paged_decode_workspace_bytes(c, d) bytes, 16-byte
+ *              aligned: Exchange scan states of the history's slices
+ * max_length bounds the lengths of this call and with them the launch and the
+ * workspace; <= 0 takes table_width * page_size. A request whose length is
+ * outside 1 .. that bound, or one of whose pages is not in the pool, gets NaN
+ * rows in out and row_stat. Entries past a request's length are not read. */
+typedef struct rel_paged_query {
+  int64_t B, Hq, table_width, max_length;
+  float tau_s, scale; /* as in rel_problem; scale <= 0: 1/sqrt(c->D) */
+} rel_paged_query;
+size_t relation_paged_decode_workspace_bytes(const rel_pages* c, const rel_paged_query* d);
+rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, const void* q, const void* k_cache,
+                                 const void* v_cache, const int32_t* table, const int32_t* lengths,
+                                 const float* lambda, void* out, float* row_stat, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* One token of each row of logits. With d_i = (x_i - max x) / T, w_i = exp(d_i),
+ * Z their sum, and the tokens in the order of falling x (equal ones: lower
+ * index first), token i is kept if it is the first, or if
+ *   fewer than top_k tokens stand before it       (top_k <= 0: no bound),
+ *   those before it weigh less than top_p Z       (top_p >= 1: no bound), and
+ *   w_i >= min_p                                  (min_p <= 0: no bound).
+ * The token is the kept one with the largest w_i / noise_i (equal ones: lower
+ * index), which is distributed as the kept w, renormalised, if noise holds
+ * independent exponential variates (values below 2^-126 count as that).
+ *   logits     [B, V] dtype, noise [B, V] fp32: element strides of the rows
+ *              below, rows contiguous. noise is read for tokens in the running only.
+ *   temperature, top_p, min_p fp32 [B], top_k int32 [B]: NULL for 1, 1, 0, 0.
+ *              T = 0 takes the first token (its logprob at T = 1).
+ *   tokens     int64 [B]   logprob  fp32 [B], optional: d_i - ln Z of the token
+ *              (before the filters)
+ *   workspace  relation_sample_workspace_bytes(s) bytes, 16-byte aligned
+ * NaN logits count as -inf. A row with nothing above -inf, with a negative or
+ * NaN temperature or a NaN filter gives token -1 and logprob NaN. V <= 2^22. */
+typedef struct rel_sample {
+  int64_t B, V;
+  int32_t dtype;
+  int64_t stride_logits, stride_noise;
+} rel_sample;
+size_t relation_sample_workspace_bytes(const rel_sample* s);
+rel_status relation_sample(const rel_sample* s, const void* logits, const float* noise, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p, int64_t* tokens,
+                           float* logprob, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid. While armed, every launch of the named kernel ("fwd": the
  * fused forward kernel; "bwd": all kernels of one relation_bwd call, back to
  * back; "bwd_dkdv": the dk/dv kernel, or the one-kernel backward's main

@@ -13,6 +13,10 @@ from .binding import (  # noqa: F401
     relation_fwd_materialized,
     relation_fwd_materialized_workspace_bytes,
     relation_exchange_allocation,
+    relation_page_map,
+    relation_paged_append,
+    relation_paged_decode,
+    relation_sample,
     load_library,
     TAU_S,
 )

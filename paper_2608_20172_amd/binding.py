@@ -37,6 +37,33 @@ class RelLayerOpts(ctypes.Structure):
     _fields_ = [("rope_base", ctypes.c_double), ("givens", ctypes.c_int32), ("transport", ctypes.c_int32)]
 
 
+class RelPages(ctypes.Structure):
+    _fields_ = [("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("D", ctypes.c_int64), ("dtype", ctypes.c_int32), ("stride_page", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("stride_token", ctypes.c_int64)]
+
+
+class RelPageMap(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("table_width", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("max_tokens", ctypes.c_int64), ("num_free", ctypes.c_int64)]
+
+
+class RelAppend(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("Hq", ctypes.c_int64), ("D", ctypes.c_int64), ("q_token", ctypes.c_int64),
+                ("q_head", ctypes.c_int64), ("kv_token", ctypes.c_int64), ("kv_head", ctypes.c_int64),
+                ("rope_base", ctypes.c_double), ("givens", ctypes.c_int32)]
+
+
+class RelPagedQuery(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("Hq", ctypes.c_int64), ("table_width", ctypes.c_int64),
+                ("max_length", ctypes.c_int64), ("tau_s", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class RelSample(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("V", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("stride_logits", ctypes.c_int64), ("stride_noise", ctypes.c_int64)]
+
+
 REL_GIVENS = {None: 0, "A": 1, "B": 2}
 REL_TRANSPORT = {"full": 0, "exchange": 1}
 ROPE_BASE = 1.0e4
@@ -83,6 +110,14 @@ _SIGS = {
     "relation_linear_gated_bwd_workspace_bytes": (ctypes.c_size_t, [_PP, ctypes.c_int32]),
     "relation_linear_gated_bwd": (ctypes.c_int, [_PP, _P, _P, _P, _P, _P, _P, ctypes.c_int32, ctypes.c_float, _P,
                                                  _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "relation_page_map": (ctypes.c_int, [ctypes.POINTER(RelPageMap)] + [_P] * 10),
+    "relation_paged_append": (ctypes.c_int, [ctypes.POINTER(RelPages), ctypes.POINTER(RelAppend)] + [_P] * 10),
+    "relation_paged_decode_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelPages),
+                                                                ctypes.POINTER(RelPagedQuery)]),
+    "relation_paged_decode": (ctypes.c_int, [ctypes.POINTER(RelPages), ctypes.POINTER(RelPagedQuery)] + [_P] * 9 +
+                              [ctypes.c_size_t, _P]),
+    "relation_sample_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelSample)]),
+    "relation_sample": (ctypes.c_int, [ctypes.POINTER(RelSample)] + [_P] * 9 + [ctypes.c_size_t, _P]),
     "relation_profile_arm": (ctypes.c_int, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]),
     "relation_profile_disarm": (ctypes.c_int, []),
     "relation_mfma_peak_flops": (ctypes.c_int64, [ctypes.c_int, ctypes.c_int]),
@@ -605,6 +640,181 @@ def relation_linear_gated_bwd(p1, p2, v, r, a_log, dt_bias, dout, *, rope_dim: i
                                        _stream())
     _check(st, "relation_linear_gated_bwd")
     return {"dp1": dp1, "dp2": dp2, "dv": dv, "dr": dr, "da_log": da_log, "ddt_bias": ddt_bias}
+
+
+# ---------------------------------------------------------------------------
+# Serving from a paged cache
+# ---------------------------------------------------------------------------
+def _on_gpu(**tensors):
+    """The device that all the given tensors (None apart) share."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{name} must be a tensor on the GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, other tensors on {dev}")
+    return dev
+
+
+def _out(out, name, shape, dtype, dev):
+    """out[name] where the caller gives it (checked), or a new tensor."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if t.shape != torch.Size(shape) or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t
+
+
+def make_pages(k_cache: torch.Tensor, v_cache: torch.Tensor) -> RelPages:
+    """The pools [num_pages, H, page_size, D], with any strides that the library takes."""
+    if k_cache.dim() != 4:
+        raise ValueError("caches must be [num_pages, H, page_size, D]")
+    shape, strides = k_cache.shape, k_cache.stride()
+    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype != k_cache.dtype:
+        raise ValueError("k_cache and v_cache must share shape, strides and dtype")
+    if strides[3] != 1 and shape[3] != 1:
+        raise ValueError("the last dimension must be contiguous")
+    P, H, page, D = shape
+    sp, sh, st = (s if n > 1 else 0 for s, n in zip(strides, shape[:3]))  # a stride over one entry says nothing
+    return RelPages(P, page, H, D, _dtype_code(k_cache.dtype), sp, sh, st)
+
+
+def relation_page_map(cached, added, table, free_pages, page_size: int, max_tokens: int, *, out=None):
+    """Block tables, slots and positions of a step. cached, added: int32 [B]; table: int32 [B, W], updated in
+    place; free_pages: int32 [F]; max_tokens: the step's token buffers. Returns dict(table, lengths [B],
+    row_start [B + 1], slots int64 [max_tokens], positions [max_tokens], counts [3]: pages taken, tokens mapped,
+    requests not served), in the tensors of ``out`` where given."""
+    lib = load_library()
+    dev = _on_gpu(cached=cached, added=added, table=table, free_pages=free_pages)
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 [B, W] tensor")
+    B, W = table.shape
+    if cached.shape != (B,) or added.shape != (B,) or free_pages.dim() != 1:
+        raise ValueError("cached and added must be [B], free_pages [F]")
+    cached, added = _dense(cached, dev, torch.int32), _dense(added, dev, torch.int32)
+    free_pages = _dense(free_pages, dev, torch.int32)
+    i32, N = torch.int32, int(max_tokens)
+    if N < 0:
+        raise ValueError("max_tokens must not be negative")
+    lengths, row_start = _out(out, "lengths", (B,), i32, dev), _out(out, "row_start", (B + 1,), i32, dev)
+    slots, positions = _out(out, "slots", (N,), torch.int64, dev), _out(out, "positions", (N,), i32, dev)
+    counts = _out(out, "counts", (3,), i32, dev)
+    m = RelPageMap(B, W, int(page_size), N, free_pages.shape[0])
+    st = lib.relation_page_map(ctypes.byref(m), _ptr(cached), _ptr(added), _ptr(free_pages), _ptr(table),
+                               _ptr(lengths), _ptr(row_start), _ptr(slots), _ptr(positions), _ptr(counts), _stream())
+    _check(st, "relation_page_map")
+    return {"table": table, "lengths": lengths, "row_start": row_start, "slots": slots, "positions": positions,
+            "counts": counts}
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    return t if t.stride(2) == 1 or t.shape[2] == 1 else t.contiguous()
+
+
+def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, theta=None,
+                          pairing: Optional[str] = None, rope_base: float = ROPE_BASE, out=None):
+    """New tokens' rows into the cache, in place: k (RoPE at the positions) and v (Givens mixing), [N, H, D], to
+    slots (int64 [N]) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc. With q [N, Hq, D], returns
+    the rotated and padded queries [N, Hq, Dc] (out["q"] where given), else None. rope_base 0 or None: no RoPE."""
+    lib = load_library()
+    dev = _on_gpu(k=k, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots, positions=positions, q=q)
+    c = make_pages(k_cache, v_cache)
+    if pairing not in REL_GIVENS:
+        raise ValueError("pairing must be None, 'A' or 'B'")
+    if k.dim() != 3 or k.shape[1] != c.H or k.dtype != k_cache.dtype:
+        raise ValueError("k and v must be [N, H, D] with the caches' heads and dtype")
+    N, H, D = k.shape
+    k = _rows(k)
+    (v,) = _same_layout(k, v)
+    if slots.shape != (N,) or positions.shape != (N,):
+        raise ValueError("slots and positions must be [N]")
+    slots, positions = _dense(slots, dev, torch.int64), _dense(positions, dev, torch.int32)
+    th = _theta_tensor(theta, H, dev)
+    if pairing is not None and th is None:
+        raise ValueError("theta is required for Givens mixing")
+    Hq = 0
+    q_out, qs = None, (0, 0)
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != N or q.shape[2] != D or q.dtype != k.dtype:
+            raise ValueError("q must be [N, Hq, D] with k's dtype")
+        q = _rows(q)
+        Hq, qs = q.shape[1], q.stride()
+        q_out = _out(out, "q", (N, Hq, c.D), q.dtype, dev)
+    ks = k.stride()
+    n = RelAppend(N, Hq, D, qs[0], qs[1], ks[0], ks[1], float(rope_base or 0.0), REL_GIVENS[pairing])
+    st = lib.relation_paged_append(ctypes.byref(c), ctypes.byref(n), _ptr(q), _ptr(k), _ptr(v), _ptr(slots),
+                                   _ptr(positions), _ptr(th), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream())
+    _check(st, "relation_paged_append")
+    return q_out
+
+
+def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_length: Optional[int] = None,
+                          tau_s: float = TAU_S, scale: Optional[float] = None, workspace=None, out=None):
+    """One decode step over pages: q [B, Hq, D] of the new tokens, caches [num_pages, H, page_size, D] (Hq a
+    multiple of H), table int32 [B, W], lengths int32 [B] (the new token's own entry last), max_length a bound of
+    the lengths (default W * page_size). Returns dict(o [B, Hq, D], row_stat [B, Hq])."""
+    lib = load_library()
+    dev = _on_gpu(q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths)
+    c = make_pages(k_cache, v_cache)
+    if q.dim() != 3 or q.shape[2] != c.D or q.dtype != k_cache.dtype:
+        raise ValueError("q must be [B, Hq, D] with the caches' width and dtype")
+    B, Hq, D = q.shape
+    if table.dim() != 2 or table.shape[0] != B or lengths.shape != (B,):
+        raise ValueError("table must be [B, W] and lengths [B]")
+    q = q.contiguous()
+    table, lengths = _dense(table, dev, torch.int32), _dense(lengths, dev, torch.int32)
+    lam_t = _lam_tensor(lam, dev)
+    d = RelPagedQuery(B, Hq, table.shape[1], int(max_length or 0), float(tau_s), 0.0 if scale is None else float(scale))
+    o = _out(out, "o", (B, Hq, D), q.dtype, dev)
+    rs = _out(out, "row_stat", (B, Hq), torch.float32, dev)
+    ws = _workspace(int(lib.relation_paged_decode_workspace_bytes(ctypes.byref(c), ctypes.byref(d))), workspace, dev)
+    st = lib.relation_paged_decode(ctypes.byref(c), ctypes.byref(d), _ptr(q), _ptr(k_cache), _ptr(v_cache),
+                                   _ptr(table), _ptr(lengths), _ptr(lam_t), _ptr(o), _ptr(rs), _ptr(ws),
+                                   0 if ws is None else _nbytes(ws), _stream())
+    _check(st, "relation_paged_decode")
+    return {"o": o, "row_stat": rs}
+
+
+def _per_row(x, name, B, dtype, dev):
+    if x is None:
+        return None
+    if not isinstance(x, torch.Tensor):
+        return torch.full((B,), x, dtype=dtype, device=dev)
+    if x.shape != (B,):
+        raise ValueError(f"{name} must be a number or [B]")
+    return _dense(x, dev, dtype)
+
+
+def relation_sample(logits, noise, *, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, out=None):
+    """One token of each row of logits [B, V], drawn by noise (fp32 [B, V], independent exponential variates).
+    temperature, top_k, top_p, min_p: numbers, [B] tensors, or None (off). Returns dict(tokens int64 [B],
+    logprob fp32 [B]: log softmax(logits / temperature) of the token)."""
+    lib = load_library()
+    dev = _on_gpu(logits=logits, noise=noise)
+    if logits.dim() != 2 or noise.shape != logits.shape or noise.dtype != torch.float32:
+        raise ValueError("logits must be [B, V] and noise fp32 [B, V]")
+    B, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        logits = logits.contiguous()
+    if V > 1 and noise.stride(1) != 1:
+        noise = noise.contiguous()
+    temperature = _per_row(temperature, "temperature", B, torch.float32, dev)
+    top_k = _per_row(top_k, "top_k", B, torch.int32, dev)
+    top_p, min_p = _per_row(top_p, "top_p", B, torch.float32, dev), _per_row(min_p, "min_p", B, torch.float32, dev)
+    s = RelSample(B, V, _dtype_code(logits.dtype), logits.stride(0), noise.stride(0))
+    tokens = _out(out, "tokens", (B,), torch.int64, dev)
+    logprob = _out(out, "logprob", (B,), torch.float32, dev)
+    ws = _workspace(int(lib.relation_sample_workspace_bytes(ctypes.byref(s))), workspace, dev)
+    st = lib.relation_sample(ctypes.byref(s), _ptr(logits), _ptr(noise), _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                             _ptr(min_p), _ptr(tokens), _ptr(logprob), _ptr(ws), 0 if ws is None else _nbytes(ws),
+                             _stream())
+    _check(st, "relation_sample")
+    return {"tokens": tokens, "logprob": logprob}
 
 
 def relation_profile_arm(kernel: str, events: list) -> None:

@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 
 ARCH = "gfx950"
 SOURCES = ["fwd.hip", "bwd.hip", "rows.hip", "layer.hip", "decode.hip", "linear.hip", "linear_bf16.hip", "measure.hip",
-           "relation_api.cpp"]
+           "pages.hip", "paged_decode.hip", "sample.hip", "relation_api.cpp", "serve_api.cpp"]
+API_SOURCES = ("relation_api.cpp", "serve_api.cpp")
 
 # Packed fp32 VALU instructions are disabled for all device code.
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -78,8 +79,8 @@ def build_host_sanitized(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     objs = []
     for src in SOURCES:
-        if src == "relation_api.cpp":
-            obj = os.path.join(BUILD_DIR, "relation_api_host_sanitized.o")
+        if src in API_SOURCES:
+            obj = os.path.join(BUILD_DIR, src[:-len(".cpp")] + "_host_sanitized.o")
             cmd = [hipcc(), *COMMON, *DEVICE_FLAGS, *HOST_SANITIZE, "-x", "hip", "-c", os.path.join(CSRC, src),
                    "-o", obj]
             r = subprocess.run(cmd, capture_output=True, text=True)

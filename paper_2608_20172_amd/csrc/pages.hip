@@ -1,0 +1,330 @@
+// Block tables and slot maps of a serving step, and the rows of its tokens
+// written into a paged cache.
+#include "kernels.h"
+#include "serve.h"
+
+namespace rel {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// Page map. With c_b tokens cached and a_b added, request b needs
+//   need_b = ceil((c_b + a_b) / p) - ceil(c_b / p)
+// pages, and takes them from the free list at the sum of the needs before it;
+// its tokens stand at the sum of the a's before it. Both sums are one scan over
+// the batch, which every workgroup makes for itself in LDS (8 bytes a request
+// read, no second launch and no pass through memory between them); then a
+// thread finds its token's request by bisection of the ends.
+// Latency-bound: a launch, two dependent reads and the scan.
+// ---------------------------------------------------------------------------
+constexpr int kMapT = 1024;
+constexpr int kMapTokens = 4;  // tokens per thread
+
+struct MapRow {
+  int64_t tokens, have, need;
+  bool valid;
+};
+
+__device__ __forceinline__ MapRow map_row(const PageMapArgs& a, int b) {
+  const int64_t c = a.cached[b], n = a.added[b], p1 = (1 << a.shift) - 1;
+  MapRow r;
+  r.tokens = n > 0 ? n : 0;
+  r.have = c > 0 ? (c + p1) >> a.shift : 0;
+  const int64_t want = (c + n + p1) >> a.shift;
+  r.valid = c >= 0 && n >= 0 && want <= a.W;
+  r.need = r.valid ? want - r.have : 0;
+  return r;
+}
+
+// end and pages: the inclusive sums of tokens and needs at this request
+__device__ __forceinline__ bool map_served(const PageMapArgs& a, const MapRow& r, int end, int pages) {
+  return r.valid && (r.tokens == 0 || end <= a.N) && (r.need == 0 || pages <= a.F);
+}
+
+// first b in [0, B) with x[b] > v (x ascending); B if none
+__device__ __forceinline__ int first_above(const int* x, int B, int v) {
+  int lo = 0, hi = B;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (x[mid] > v)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kMapT) void page_map_kernel(PageMapArgs a) {
+  extern __shared__ int lds[];
+  int* end = lds;           // [B] sums of tokens, held to 2^31 - 1 (N is less)
+  int* pages = lds + a.B;   // [B] sums of needs, held likewise
+  __shared__ int64_t wsum[2][kMapT / 64];
+  __shared__ int total[3];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int per = (a.B + kMapT - 1) / kMapT;
+  const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  int64_t t = 0, n = 0;
+  for (int b = b0; b < b1; ++b) {
+    const MapRow r = map_row(a, b);
+    t += r.tokens;
+    n += r.need;
+  }
+  const int64_t t0 = t, n0 = n;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t tt = __shfl_up(t, o, 64), nn = __shfl_up(n, o, 64);
+    if (lane >= o) {
+      t += tt;
+      n += nn;
+    }
+  }
+  if (lane == 63) {
+    wsum[0][w] = t;
+    wsum[1][w] = n;
+  }
+  if (tid < 3) total[tid] = 0;
+  __syncthreads();
+  t -= t0;
+  n -= n0;
+  for (int x = 0; x < w; ++x) {
+    t += wsum[0][x];
+    n += wsum[1][x];
+  }
+  for (int b = b0; b < b1; ++b) {
+    const MapRow r = map_row(a, b);
+    t += r.tokens;
+    n += r.need;
+    end[b] = (int)(t < 0x7fffffff ? t : 0x7fffffff);
+    pages[b] = (int)(n < 0x7fffffff ? n : 0x7fffffff);
+  }
+  __syncthreads();
+
+  // the requests' own values: the first workgroup
+  if (blockIdx.x == 0) {
+    int taken = 0, mapped = 0, refused = 0;
+    for (int b = tid; b < a.B; b += kMapT) {
+      const MapRow r = map_row(a, b);
+      const bool s = map_served(a, r, end[b], pages[b]);
+      a.lengths[b] = s ? a.cached[b] + a.added[b] : 0;
+      a.row_start[b + 1] = min(end[b], a.N);
+      if (s) {
+        taken += (int)r.need;
+        mapped += (int)r.tokens;
+      } else {
+        ++refused;
+      }
+    }
+    if (tid == 0) a.row_start[0] = 0;
+    atomicAdd(&total[0], taken);
+    atomicAdd(&total[1], mapped);
+    atomicAdd(&total[2], refused);
+    __syncthreads();
+    if (tid < 3) a.counts[tid] = total[tid];
+  }
+
+  // pages taken, in the order of the free list
+  const int64_t stride = (int64_t)gridDim.x * kMapT, first = (int64_t)blockIdx.x * kMapT + tid;
+  const int avail = a.B ? min(pages[a.B - 1], a.F) : 0;
+  for (int64_t i = first; i < avail; i += stride) {
+    const int b = first_above(pages, a.B, (int)i);
+    const MapRow r = map_row(a, b);
+    if (map_served(a, r, end[b], pages[b]))
+      a.table[(int64_t)b * a.W + r.have + (i - (pages[b] - r.need))] = a.free_pages[i];
+  }
+
+  // tokens
+  for (int64_t i = first; i < a.N; i += stride) {
+    int64_t slot = -1;
+    int pos = -1;
+    const int b = first_above(end, a.B, (int)i);
+    if (b < a.B) {
+      const MapRow r = map_row(a, b);
+      if (map_served(a, r, end[b], pages[b])) {
+        pos = (int)(a.cached[b] + (i - (end[b] - r.tokens)));
+        const int j = pos >> a.shift;
+        // a page of this step is read from the free list: its table entry may not be written yet
+        const int64_t id = j < r.have ? a.table[(int64_t)b * a.W + j] : a.free_pages[pages[b] - r.need + (j - r.have)];
+        slot = id * (1 << a.shift) + (pos & ((1 << a.shift) - 1));
+      }
+    }
+    a.slots[i] = slot;
+    a.positions[i] = pos;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows into the cache. One workgroup takes `tpw` tokens: cos and sin of their
+// channel pairs go to LDS once (the angle in 64-bit turns, so that a long
+// context keeps its fraction), then the rows of all heads are moved by threads
+// that hold a chunk of the first half and the one it turns with. Every channel
+// is read and written once: bound by memory.
+// ---------------------------------------------------------------------------
+constexpr int kAppT = 256;
+constexpr int kAppMaxTokens = 16;
+
+template <typename TI, int VEC>
+__device__ __forceinline__ void load_vec(const TI* p, float (&x)[VEC]) {
+  if constexpr (VEC == 1) {
+    x[0] = (float)*p;
+  } else if constexpr (sizeof(TI) == 2) {  // pairs from whole words
+    typedef unsigned int U __attribute__((ext_vector_type(VEC / 2 > 1 ? VEC / 2 : 2)));
+    if constexpr (VEC == 2) {
+      const unsigned int u = *reinterpret_cast<const unsigned int*>(p);
+      x[0] = bf16_lo(u);
+      x[1] = bf16_hi(u);
+    } else {
+      const U u = *reinterpret_cast<const U*>(p);
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        x[2 * e] = bf16_lo(u[e]);
+        x[2 * e + 1] = bf16_hi(u[e]);
+      }
+    }
+  } else {
+    typedef TI V __attribute__((ext_vector_type(VEC)));
+    const V u = *reinterpret_cast<const V*>(p);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = u[e];
+  }
+}
+template <typename TI, int VEC>
+__device__ __forceinline__ void store_vec(TI* p, const float (&x)[VEC]) {
+  typedef TI V __attribute__((ext_vector_type(VEC)));
+  if constexpr (VEC == 1) {
+    *p = (TI)x[0];
+  } else {
+    V u;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) u[e] = (TI)x[e];
+    *reinterpret_cast<V*>(p) = u;
+  }
+}
+
+template <typename TI, int VEC>
+__global__ __launch_bounds__(kAppT) void append_kernel(AppendArgs a, int tpw) {
+  extern __shared__ float2 cs[];  // [tpw][D / 2]
+  __shared__ int64_t row0[kAppMaxTokens];  // cache offset of the token's first head, or -1: not written
+  const int tid = threadIdx.x;
+  const int n0 = blockIdx.x * tpw, nt = min(tpw, a.N - n0);
+  const int half = a.D >> 1, Dc = a.c.D;
+  if (tid < nt) {
+    const int64_t slot = a.slots[n0 + tid];
+    const bool in = a.positions[n0 + tid] >= 0 && slot >= 0 && (slot >> a.c.shift) < a.c.num_pages;
+    row0[tid] = in ? (slot >> a.c.shift) * a.c.sp + (slot & ((1 << a.c.shift) - 1)) * (int64_t)a.c.st : -1;
+  }
+  if (a.rope) {
+    for (int i = tid; i < nt * half; i += kAppT) {
+      const int n = i / half, j = i - n * half;
+      const double x = (double)a.positions[n0 + n] * a.turns[j];
+      const float f = (float)(2.0 * (x - rint(x)));  // half turns in [-1, 1]
+      float s, c;
+      sincospif(f, &s, &c);
+      cs[i] = make_float2(c, s);
+    }
+  }
+  __syncthreads();
+  const int nq = a.q ? a.Hq : 0, heads = nq + a.c.H;
+  // q and k: tasks (token, head, chunk of the first part); without RoPE the parts are chunks VEC apart
+  const int ch = a.rope ? half / VEC : a.D / VEC;  // chunks per row
+  for (int i = tid; i < nt * heads * ch; i += kAppT) {
+    const int c = i % ch, nh = i / ch, h = nh % heads, n = nh / heads;
+    const bool isq = h < nq;
+    const int64_t r0 = row0[n];
+    if (!isq && r0 < 0) continue;
+    const int hk = h - nq;
+    const TI* src = isq ? (const TI*)a.q + (n0 + n) * a.q_token + h * a.q_head
+                        : (const TI*)a.k + (n0 + n) * a.kv_token + hk * a.kv_head;
+    TI* dst = isq ? (TI*)a.q_out + ((int64_t)(n0 + n) * a.Hq + h) * Dc : (TI*)a.k_cache + r0 + (int64_t)hk * a.c.sh;
+    const int e0 = c * VEC;
+    float x[VEC], y[VEC];
+    load_vec<TI, VEC>(src + e0, x);
+    if (a.rope) {
+      load_vec<TI, VEC>(src + half + e0, y);
+      float u[VEC], v[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float2 t = cs[n * half + e0 + e];
+        u[e] = x[e] * t.x - y[e] * t.y;
+        v[e] = x[e] * t.y + y[e] * t.x;
+      }
+      if (r0 < 0) {  // a token of no request
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e] = v[e] = 0.0f;
+      }
+      store_vec<TI, VEC>(dst + e0, u);
+      store_vec<TI, VEC>(dst + half + e0, v);
+    } else {
+      if (r0 < 0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = 0.0f;
+      }
+      store_vec<TI, VEC>(dst + e0, x);
+    }
+  }
+  // v: a head pair's chunk with Givens mixing, else one head's
+  const int vch = a.D / VEC, vh = a.givens ? a.c.H / 2 : a.c.H;
+  for (int i = tid; i < nt * vh * vch; i += kAppT) {
+    const int c = i % vch, nh = i / vch, h = nh % vh, n = nh / vh;
+    const int64_t r0 = row0[n];
+    if (r0 < 0) continue;
+    const TI* src = (const TI*)a.v + (n0 + n) * a.kv_token + c * VEC;
+    TI* dst = (TI*)a.v_cache + r0 + c * VEC;
+    float x[VEC], y[VEC];
+    if (a.givens) {
+      const int p = 2 * h + (a.givens == 2 ? 1 : 0), p2 = p + 1 == a.c.H ? 0 : p + 1;
+      float sn, cn;
+      sincosf(a.theta[h], &sn, &cn);
+      load_vec<TI, VEC>(src + p * a.kv_head, x);
+      load_vec<TI, VEC>(src + p2 * a.kv_head, y);
+      float u[VEC], v[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        u[e] = cn * x[e] - sn * y[e];
+        v[e] = sn * x[e] + cn * y[e];
+      }
+      store_vec<TI, VEC>(dst + (int64_t)p * a.c.sh, u);
+      store_vec<TI, VEC>(dst + (int64_t)p2 * a.c.sh, v);
+    } else {
+      load_vec<TI, VEC>(src + h * a.kv_head, x);
+      store_vec<TI, VEC>(dst + (int64_t)h * a.c.sh, x);
+    }
+  }
+  // zeros in channels D .. Dc - 1
+  const int pad = Dc - a.D, ph = nq + 2 * a.c.H;
+  for (int i = tid; i < nt * ph * pad; i += kAppT) {
+    const int e = a.D + i % pad, nh = i / pad, h = nh % ph, n = nh / ph;
+    const int64_t r0 = row0[n];
+    if (h < nq)
+      ((TI*)a.q_out)[((int64_t)(n0 + n) * a.Hq + h) * Dc + e] = (TI)0.0f;
+    else if (r0 >= 0)
+      (h < nq + a.c.H ? (TI*)a.k_cache + (int64_t)(h - nq) * a.c.sh : (TI*)a.v_cache + (int64_t)(h - nq - a.c.H) * a.c.sh)
+          [r0 + e] = (TI)0.0f;
+  }
+}
+
+template <typename TI, int VEC>
+hipError_t append_t(const AppendArgs& a, hipStream_t stream) {
+  const int tpw = a.N >= 4096 ? 8 : 1;
+  hipLaunchKernelGGL((append_kernel<TI, VEC>), dim3((unsigned)((a.N + tpw - 1) / tpw)), dim3(kAppT),
+                     (size_t)tpw * (a.D / 2) * sizeof(float2), stream, a, tpw);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
+  const int64_t want = ((int64_t)a.N + kMapT * kMapTokens - 1) / (kMapT * kMapTokens);
+  const unsigned grid = (unsigned)(want < 1 ? 1 : want > 2048 ? 2048 : want);
+  hipLaunchKernelGGL(page_map_kernel, dim3(grid), dim3(kMapT), (size_t)a.B * 8, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_append(const AppendArgs& a, int dtype, int vec, hipStream_t stream) {
+  if (dtype == 1) {
+    if (vec == 8) return append_t<bf16, 8>(a, stream);
+    return vec == 2 ? append_t<bf16, 2>(a, stream) : append_t<bf16, 1>(a, stream);
+  }
+  if (vec == 4) return append_t<float, 4>(a, stream);
+  return vec == 2 ? append_t<float, 2>(a, stream) : append_t<float, 1>(a, stream);
+}
+
+}  // namespace rel

@@ -14,6 +14,7 @@
 #include <string>
 #include <vector>
 
+#include "api.h"
 #include "kernels.h"
 
 namespace {
@@ -332,6 +333,42 @@ std::vector<hipEvent_t> g_prof_events;
 int g_prof_next = 0;
 
 }  // namespace
+
+rel_status rel::api_fail(rel_status s, const char* fmt, ...) noexcept {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  try {
+    g_last_error = buf;
+  } catch (...) {  // no memory for the message: the status alone goes back
+  }
+  return s;
+}
+
+bool rel::api_fail_launch() noexcept { return test_fail_launch(); }
+
+static Lattice sorted_lattice(const rel::ApiLattice& a) {
+  Lattice L;
+  int idx[3] = {0, 1, 2};
+  std::sort(idx, idx + 3, [&](int x, int y) { return a.stride[x] > a.stride[y]; });
+  for (int i = 0; i < 3; ++i) {
+    L.stride[i] = a.stride[idx[i]];
+    L.count[i] = a.count[idx[i]];
+  }
+  L.stride[3] = 1;
+  L.count[3] = a.width;
+  return L;
+}
+
+bool rel::api_nested(const ApiLattice& a) noexcept { return nested(sorted_lattice(a)); }
+
+bool rel::api_alias(const ApiLattice& a, const void* x, const void* y, size_t elem) noexcept {
+  const int64_t delta = (int64_t)((intptr_t)y - (intptr_t)x);
+  if (delta % (int64_t)elem != 0) return true;
+  return representable(sorted_lattice(a), 0, delta / (int64_t)elem);
+}
 
 bool rel::profile_slot(const char* name, hipEvent_t* start, hipEvent_t* stop) {
   std::lock_guard<std::mutex> lock(g_prof_mu);
