@@ -542,8 +542,9 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  *   tokens     int64 [B]   logprob  fp32 [B], optional: d_i - ln Z of the token
  *              (before the filters)
  *   workspace  relation_sample_workspace_bytes(s) bytes, 16-byte aligned
- * NaN logits count as -inf. A row with nothing above -inf, with a negative or
- * NaN temperature or a NaN filter gives token -1 and logprob NaN. V <= 2^22. */
+ * NaN logits count as -inf; w is 0 at -inf, and below +inf, whatever T. A row with nothing above -inf, with a negative or
+ * NaN temperature or a NaN filter gives token -1 and logprob NaN.
+ * V <= 2^22, B <= 2^20, B V <= 2^36. */
 typedef struct rel_sample {
   int64_t B, V;
   int32_t dtype;

@@ -113,8 +113,8 @@ def sample(x, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if not (temperature >= 0) or math.isnan(top_p) or math.isnan(min_p) or top == -np.inf:
         return {"token": -1, "logprob": math.nan, "kept": [], "lead": math.inf}
     T, k = (1.0, 1) if temperature == 0 else (float(temperature), int(top_k) if top_k > 0 else len(x))
-    with np.errstate(invalid="ignore", over="ignore"):
-        d = np.where(x == top, 0.0, (x - top) / T)
+    with np.errstate(invalid="ignore", over="ignore"):  # -inf, and what is finite beside +inf, weighs nothing at any T
+        d = np.where(x == top, 0.0, np.where(x - top == -np.inf, -np.inf, (x - top) / T))
     w = np.exp(d)
     Z = math.fsum(w)
     order = np.lexsort((np.arange(len(x)), -x))  # falling x, then the index

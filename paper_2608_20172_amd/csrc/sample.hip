@@ -8,9 +8,19 @@
 // before it, they weigh less than top_p Z, and w_i >= min_p. The token drawn is
 // the kept one with the largest w_i / r_i (r_i exponential: a race that token i
 // wins with probability w_i / sum of the kept w). So the race is run over all
-// tokens, its winner is looked up in the order by one sum over the row, and if it
-// is not kept, nothing after it is either, and the race is run again over the
-// tokens before it. The sum and the next race are one pass.
+// tokens, its winner is looked up in the order by one sum, and if it is not kept,
+// nothing after it is either, and the race is run again over the tokens before
+// it. The sum and the next race are one pass.
+//
+// The logits are read once, by many workgroups a row (scan): each holds its chunk
+// in registers, and leaves the chunk's maximum, its sum of exponentials, and for
+// a row without filters the winner of its race. For a row with filters it lists
+// its largest logits: all at or above a bound tau that about kTarget tokens of
+// the row pass. One workgroup a row (pick) then joins the chunks; the tokens at
+// or above the largest tau are all in the lists, and where the filters' bound is
+// reached among them, the rounds run over the lists in registers, with r read for
+// those tokens alone. Otherwise (flat rows, many equal logits) they run over the
+// row. Sums are in fp32 and in an order that the sizes alone give.
 #include "kernels.h"
 #include "serve.h"
 
@@ -18,14 +28,31 @@ namespace rel {
 
 namespace {
 
-constexpr int kSampleT = 1024;
+constexpr int kScanT = 256, kPickT = 512;
+constexpr int kListCap = 512;  // listed tokens of a chunk
+constexpr int kTarget = 2048;  // listed tokens of a row, about
+constexpr int kHeld = 12;      // listed tokens that a thread of pick holds
+constexpr int kCutBits = 12;   // low bits of the ordered logit that the bound tau leaves out
 constexpr float kTiny = 1.17549435e-38f;  // random numbers count as at least 2^-126
+constexpr float kFltMax = 3.402823466e+38f;
+
+// What the scan leaves of a chunk.
+struct Part {
+  float m;       // largest logit, and the first token that has it
+  int mi;
+  float z;       // sum of exp((x - m) / T)
+  float tau;     // all tokens at or above are listed
+  int n;         // listed tokens; -1: no list
+  int wi;        // winner of the chunk's race (0x7fffffff: not run), its logit and random number
+  float wx, wr;
+};
 
 struct RowParams {
   float T, top_p, min_p;
-  int k;        // V where the filter is off
-  bool greedy;  // the first token
-  bool bad;     // a parameter outside its range: token -1
+  int k;          // V where the filter is off
+  bool greedy;    // the first token
+  bool bad;       // a parameter outside its range: token -1
+  bool filtered;  // some filter may leave tokens out
 };
 __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int b) {
   RowParams p;
@@ -34,142 +61,627 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int b) {
   p.top_p = a.top_p ? a.top_p[b] : 1.0f;
   p.min_p = a.min_p ? a.min_p[b] : 0.0f;
   p.bad = !(p.T >= 0.0f) || p.top_p != p.top_p || p.min_p != p.min_p;
-  p.greedy = p.T == 0.0f;
-  if (p.greedy) p.T = 1.0f;
   if (p.k <= 0 || p.k > a.V) p.k = a.V;
+  p.greedy = p.T == 0.0f || p.k == 1;
+  if (p.T == 0.0f) p.T = 1.0f;
+  p.filtered = p.k < a.V || p.top_p < 1.0f || p.min_p > 0.0f;
   return p;
 }
 
-__device__ __forceinline__ float logit(const bf16* p, int64_t i) { return (float)p[i]; }
-__device__ __forceinline__ float logit(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : kNegInf; }
 
-// w of logit x: 1 for the largest, also where that is infinite
-__device__ __forceinline__ float exponent(float x, float top, float T) { return x == top ? 0.0f : (x - top) / T; }
+// Loads of 16 bytes, on any element boundary: raw first, so that a run of them is in flight together.
+template <typename TI>
+struct Logits;
+template <>
+struct Logits<float> {
+  static constexpr int VE = 4;
+  typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void values(const V& u, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = no_nan(u[e]);
+  }
+};
+template <>
+struct Logits<bf16> {
+  static constexpr int VE = 8;
+  typedef unsigned int V __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ void values(const V& u, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = no_nan(bf16_lo(u[e]));
+      x[2 * e + 1] = no_nan(bf16_hi(u[e]));
+    }
+  }
+};
+// N runs of VE elements of a row of V: run s is wanted from at[s] on. Where it
+// would pass the row's end it is the row's last VE elements (at[s] becomes their
+// first), and those before the wanted ones, which another run has, are -inf.
+template <typename TI, int N>
+__device__ __forceinline__ void load_runs(const TI* row, int V, int (&at)[N], float (&x)[N][Logits<TI>::VE]) {
+  constexpr int VE = Logits<TI>::VE;
+  if (V >= VE) {
+    typename Logits<TI>::V raw[N];
+    int want[N];
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      want[s] = at[s];
+      at[s] = min(at[s], V - VE);
+      raw[s] = *reinterpret_cast<const typename Logits<TI>::V*>(row + at[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      Logits<TI>::values(raw[s], x[s]);
+      if (__any(want[s] != at[s])) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+          if (at[s] + e < want[s]) x[s][e] = kNegInf;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) x[s][e] = at[s] + e < V ? no_nan((float)row[at[s] + e]) : kNegInf;
+    }
+  }
+}
+// The random numbers of such runs; 1 past the end of a row shorter than one.
+template <int N, int VE>
+__device__ __forceinline__ void load_noise(const float* row, int V, const int (&at)[N], float (&r)[N][VE]) {
+  typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+  if (V >= VE) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+#pragma unroll
+      for (int q = 0; q < VE / 4; ++q) {
+        const F4 u = *reinterpret_cast<const F4*>(row + at[s] + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[s][4 * q + e] = u[e];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) r[s][e] = at[s] + e < V ? row[at[s] + e] : 1.0f;
+    }
+  }
+}
 
-// The larger of two (value, index) pairs; equal values: the lower index.
+// exp((x - top) / T) with log2(e) / T as hi + lo, so that the exponent keeps its fp32 accuracy however large.
+struct Scale {
+  float hi, lo;
+};
+__device__ __forceinline__ Scale scale_of(float T) {
+  const double c = 1.4426950408889634074 / (double)T;
+  Scale s;
+  s.hi = (float)c;
+  s.lo = s.hi < 3.0e38f ? (float)(c - (double)s.hi) : 0.0f;
+  return s;
+}
+__device__ __forceinline__ float weight(float x, float top, Scale s) {
+  const float t = x - top, y = t * s.hi;
+  const float e = __builtin_fmaf(t, s.hi, -y) + t * s.lo, p = fast_exp2(y);
+  // 1 for the largest, also where that is infinite; 0 for -inf, and where the exponent is past fp32's
+  return x == top ? 1.0f : y > -150.0f ? __builtin_fmaf(p, e * kLn2, p) : 0.0f;
+}
+// The same to the rounding of the exponent (2^-23 of it, either way): for sums of
+// many. min and max pass over the NaN of inf - inf (1) and of 0 inf (0).
+__device__ __forceinline__ float weight_fast(float x, float top, Scale s) {
+  const float t = fminf(x - top, 0.0f);
+  return fast_exp2(fmaxf(__builtin_fmaf(t, s.lo, t * s.hi), -1000.0f));
+}
+__device__ __forceinline__ float race(float w, float r) { return w / fmaxf(r, kTiny); }
+
+// Bits in the order of the numbers, and back.
+__device__ __forceinline__ unsigned ordered(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(unsigned u) {
+  return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+constexpr unsigned kLowest = 0x00800000u;  // ordered(-FLT_MAX)
+
+// A token in a race: the larger v wins, equal ones by the lower index. x: its logit.
 struct Best {
   float v;
   int i;
+  float x;
 };
-__device__ __forceinline__ Best better(Best a, Best b) {
-  return b.v > a.v || (b.v == a.v && b.i < a.i) ? b : a;
+constexpr Best kNobody = {-1.0f, 0x7fffffff, kNegInf};
+__device__ __forceinline__ Best better(Best a, Best b) { return b.v > a.v || (b.v == a.v && b.i < a.i) ? b : a; }
+
+// Reductions over a wave whose result every lane has: lane moves inside rows of
+// 16 on the vector unit, then two exchanges across the rows.
+template <int CTRL>
+__device__ __forceinline__ int dpp_word(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, false);
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_reduce(T x, F join) {
+  static_assert(sizeof(T) % 4 == 0, "whole words");
+  struct Words {
+    int w[sizeof(T) / 4];
+  };
+  auto moved = [&](auto move) __attribute__((always_inline)) {
+    Words u = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (unsigned k = 0; k < sizeof(T) / 4; ++k) u.w[k] = move(u.w[k]);
+    return __builtin_bit_cast(T, u);
+  };
+  x = join(x, moved([](int y) { return dpp_word<0xB1>(y); }));   // lane ^ 1
+  x = join(x, moved([](int y) { return dpp_word<0x4E>(y); }));   // lane ^ 2
+  x = join(x, moved([](int y) { return dpp_word<0x141>(y); }));  // lane i <-> 7 - i of its 8
+  x = join(x, moved([](int y) { return dpp_word<0x140>(y); }));  // lane i <-> 15 - i of its 16
+  x = join(x, moved([](int y) { return __shfl_xor(y, 16, 64); }));
+  return join(x, moved([](int y) { return __shfl_xor(y, 32, 64); }));
 }
 __device__ __forceinline__ Best wave_best(Best x) {
-  for (int o = 32; o >= 1; o >>= 1) x = better(x, Best{__shfl_xor(x.v, o, 64), __shfl_xor(x.i, o, 64)});
-  return x;
+  return wave_reduce(x, [](Best a, Best b) { return better(a, b); });
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return wave_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  return wave_reduce(x, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ int wave_sum(int x) {
+  return wave_reduce(x, [](int a, int b) { return a + b; });
 }
 
-template <typename TI>
-__global__ __launch_bounds__(kSampleT) void sample_rows_kernel(SampleArgs a) {
-  constexpr int NW = kSampleT / 64;
-  __shared__ float sv[NW], sm[NW];
-  __shared__ int si[NW], sc[NW];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const TI* x = (const TI*)a.logits + (int64_t)b * a.sl;
-  const float* r = a.noise + (int64_t)b * a.sn;
-  const RowParams p = row_params(a, b);
+// First logit of run v of chunk c of nch: the chunk has every nch-th piece of 128
+// bytes (8 runs of 16 bytes), so that tokens that stand together in the
+// vocabulary (often those of like frequency) are spread over the chunks.
+template <int VE>
+__device__ __forceinline__ int run_start(int v, int c, int nch) {
+  return (((v >> 3) * nch + c) * 8 + (v & 7)) * VE;
+}
 
-  auto block_best = [&](Best v) __attribute__((always_inline)) {
-    v = wave_best(v);
+// One chunk of one row: S loads of 16 bytes a thread, S * 4 KB in all. Every
+// fourth piece goes to a wave, for the same spread.
+// The bound tau is the least of the waves' rank-th largest thread maxima (64 a
+// wave), so that about 4 rank tokens pass it; where more do than the list holds
+// (several large ones in a thread), rank is cut to a quarter and again. A chunk
+// whose list weighs less than top_p of it belongs, most likely, to a row whose
+// kept tokens are too many for lists: it runs its race here as well, with the
+// whole chip, and spares the one workgroup of pick that.
+template <typename TI, int S>
+__global__ __launch_bounds__(kScanT, 4) void sample_scan_kernel(SampleArgs a, int nch, int rank, int cap, Part* parts,
+                                                                float2* lists) {
+  constexpr int VE = Logits<TI>::VE, NW = kScanT / 64;
+  __shared__ float tops[NW], zs[2][NW], vs[NW];
+  __shared__ unsigned cut[2][NW];
+  __shared__ int cnt[2][NW];
+  __shared__ int first;
+  __shared__ unsigned long long winner;
+  const int c = blockIdx.x % nch, b = blockIdx.x / nch;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const TI* row = (const TI*)a.logits + (int64_t)b * a.sl;
+  const float* noise = a.noise + (int64_t)b * a.sn;
+  const RowParams p = row_params(a, b);
+  const bool listed = !p.greedy && p.filtered && !p.bad;
+  float x[S][VE];
+  int at[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    at[s] = run_start<VE>(s * kScanT + (((lane >> 3) * NW + w) << 3) + (lane & 7), c, nch);
+  load_runs<TI, S>(row, a.V, at, x);
+  float own = kNegInf;
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) own = fmaxf(own, x[s][e]);
+  const unsigned mine = ordered(own);
+  // the rank-th largest of the wave's maxima, cut to its high bits
+  auto wave_cut = [&](int r) __attribute__((always_inline)) {
+    unsigned t = 0;
+#pragma unroll 1
+    for (unsigned bit = 1u << 31; bit >= 1u << kCutBits; bit >>= 1) {
+      if (__popcll(__ballot(mine >= (t | bit))) >= r) t |= bit;
+    }
+    return t;
+  };
+  const float wtop = wave_max(own);
+  const unsigned c0 = listed ? wave_cut(rank) : 0;
+  if (lane == 0) {
+    tops[w] = wtop;
+    cut[0][w] = c0;
+  }
+  if (tid == 0) {
+    first = 0x7fffffff;
+    winner = 0;
+  }
+  __syncthreads();
+  float top = tops[0];
+#pragma unroll
+  for (int k = 1; k < NW; ++k) top = fmaxf(top, tops[k]);
+  const Scale sc = scale_of(p.T);
+  if (own == top && top > kNegInf) {  // the first token that has it: the least index, whatever the order of arrival
+    int i = 0x7fffffff;
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s)
+#pragma unroll
+      for (int e = VE - 1; e >= 0; --e)
+        if (x[s][e] == top) i = at[s] + e;
+    atomicMin(&first, i);
+  }
+  float tau = 0.0f;
+  int total = 0;
+  if (listed) {
+    int turn = 0;
+    for (int r = rank;;) {
+      // a wave without so many numbers above -inf has no say; where none has one, all are listed
+      unsigned t = 0xffffffffu;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) t = min(t, cut[turn][k] < kLowest ? 0xffffffffu : cut[turn][k]);
+      tau = t == 0xffffffffu ? -kFltMax : unordered(t);
+      int n = 0;
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) n += x[s][e] >= tau;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 63) cnt[turn][w] = incl;
+      __syncthreads();
+      total = 0;
+      int before = incl - n;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        if (k < w) before += cnt[turn][k];
+        total += cnt[turn][k];
+      }
+      if (total <= cap) {  // places in the order of (wave, lane, own): the list is the same in every run
+        if (n) {
+          float2* list = lists + ((int64_t)b * nch + c) * kListCap;
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int e = 0; e < VE; ++e)
+              if (x[s][e] >= tau) list[before++] = float2{x[s][e], __builtin_bit_cast(float, at[s] + e)};
+        }
+        break;
+      }
+      if (r == 1) {
+        total = -1;
+        tau = __builtin_inff();
+        break;
+      }
+      r = max(1, r >> 2);
+      turn ^= 1;
+      const unsigned cn = wave_cut(r);
+      if (lane == 0) cut[turn][w] = cn;
+      __syncthreads();
+    }
+  }
+  float z = 0.0f, zl = 0.0f;  // the chunk's weight, and that of its listed tokens
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float wt = weight_fast(x[s][e], top, sc);
+      z += wt;
+      if (listed) zl += x[s][e] >= tau ? wt : 0.0f;
+    }
+  z = wave_sum(z);
+  zl = wave_sum(zl);
+  if (lane == 0) {
+    zs[0][w] = z;
+    zs[1][w] = zl;
+  }
+  __syncthreads();
+  z = zl = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    z += zs[0][k];
+    zl += zs[1][k];
+  }
+  const bool open = p.k >= a.V && !(p.top_p < 1.0f && zl >= p.top_p * z) && !(p.min_p > 0.0f && weight(tau, top, sc) < p.min_p);
+  const bool racing = top > kNegInf && !p.greedy && !p.bad && (!p.filtered || open);
+  if (racing) {
+    float v[S][VE], vmax = -1.0f;
+    load_noise<S, VE>(noise, a.V, at, v);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        v[s][e] = weight_fast(x[s][e], top, sc) * fast_rcp(fmaxf(v[s][e], kTiny));
+        vmax = fmaxf(vmax, v[s][e]);
+      }
+    const float wmax = wave_max(vmax);
+    if (lane == 0) vs[w] = wmax;
     __syncthreads();
-    if (lane == 0) {
-      sv[w] = v.v;
-      si[w] = v.i;
+    float near = vs[0];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) near = fmaxf(near, vs[k]);
+    near *= 1.0f - 3.0e-5f;
+    if (vmax >= near) {  // the few that come near the best are compared without the approximations
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+          if (v[s][e] >= near && x[s][e] > kNegInf) {
+            const unsigned long long bits = __builtin_bit_cast(unsigned, race(weight(x[s][e], top, sc), noise[at[s] + e]));
+            atomicMax(&winner, bits << 32 | (unsigned)(0x7fffffff - (at[s] + e)));
+          }
     }
     __syncthreads();
-    Best all{sv[0], si[0]};
+  }
+  if (tid == 0) {
+    Part part{top, first, z, tau, total, 0x7fffffff, kNegInf, 1.0f};
+    if (racing) {
+      part.wi = 0x7fffffff - (int)(winner & 0x7fffffff);
+      part.wx = no_nan((float)row[part.wi]);
+      part.wr = noise[part.wi];
+    }
+    parts[(int64_t)b * nch + c] = part;
+  }
+}
+
+// One round over some tokens: how many stand before the pivot, their weight, and the winner of the race among them.
+struct Round {
+  Best win;
+  int n;
+  float mass;
+};
+
+// Joins a row's chunks. `group` threads (a power of two) load a chunk's list,
+// kHeld tokens each at most, before it is known how long it is.
+template <typename TI>
+__global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int nch, int group, const Part* parts,
+                                                             const float2* lists) {
+  constexpr int NW = kPickT / 64, VE = Logits<TI>::VE;
+  constexpr int kAhead = 32 / VE;  // loads of 16 bytes in flight where the row is read
+  __shared__ Round rounds[2][NW];
+  __shared__ float taus[NW];
+  __shared__ unsigned char stale[kPickT];  // of a chunk: its race is to be run (again)
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const TI* row = (const TI*)a.logits + (int64_t)b * a.sl;
+  const float* noise = a.noise + (int64_t)b * a.sn;
+  parts += (int64_t)b * nch;
+  lists += (int64_t)b * nch * kListCap;
+  const int lc = min(tid / group, nch - 1), j0 = tid % group;
+  const Part mine = parts[min(tid, nch - 1)];
+  const int ln = tid / group < nch ? parts[lc].n : 0;
+  const RowParams p = row_params(a, b);
+  const bool choose = !p.greedy && p.filtered;
+  float x[kHeld];
+  int id[kHeld];
+  if (choose) {
 #pragma unroll
-    for (int k = 1; k < NW; ++k) all = better(all, Best{sv[k], si[k]});
-    return all;
-  };
-  auto block_sum = [&](float v) __attribute__((always_inline)) {
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int k = 0; k < kHeld; ++k) {
+      const float2 e = lists[(int64_t)lc * kListCap + min(j0 + k * group, kListCap - 1)];
+      x[k] = e.x;
+      id[k] = __builtin_bit_cast(int, e.y);
+    }
+  }
+  const Scale sc = scale_of(p.T);
+
+  int turn = 0;  // the reductions take two sets of LDS in turn: one barrier each
+  auto reduce = [&](Round r) __attribute__((always_inline)) {
+    r.win = wave_best(r.win);
+    r.n = wave_sum(r.n);
+    r.mass = wave_sum(r.mass);
+    if (lane == 0) rounds[turn][w] = r;
     __syncthreads();
-    if (lane == 0) sm[w] = v;
-    __syncthreads();
-    float s = 0.0f;
+    r = rounds[turn][0];
 #pragma unroll
-    for (int k = 0; k < NW; ++k) s += sm[k];
-    return s;
-  };
-  auto block_count = [&](int v) __attribute__((always_inline)) {
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    __syncthreads();
-    if (lane == 0) sc[w] = v;
-    __syncthreads();
-    int s = 0;
-#pragma unroll
-    for (int k = 0; k < NW; ++k) s += sc[k];
-    return s;
+    for (int k = 1; k < NW; ++k) {
+      const Round q = rounds[turn][k];
+      r.win = better(r.win, q.win);
+      r.n += q.n;
+      r.mass += q.mass;
+    }
+    turn ^= 1;
+    return r;
   };
 
-  Best top{kNegInf, 0x7fffffff};
-  for (int i = tid; i < a.V; i += kSampleT) top = better(top, Best{no_nan(logit(x, i)), i});
-  top = block_best(top);
-  if (p.bad || top.v == kNegInf) {  // uniform: nothing to choose from
+  // the row's first token, the bound above which all tokens are listed, and whether a chunk has no list (n)
+  Round r0{{mine.m, mine.mi, mine.m}, mine.n < 0, 0.0f};
+  float tau = mine.tau;
+  for (int c = tid + kPickT; c < nch; c += kPickT) {
+    r0.win = better(r0.win, Best{parts[c].m, parts[c].mi, parts[c].m});
+    r0.n += parts[c].n < 0;
+    tau = fmaxf(tau, parts[c].tau);
+  }
+  tau = wave_max(tau);
+  if (lane == 0) taus[w] = tau;
+  r0 = reduce(r0);
+#pragma unroll
+  for (int k = 0; k < NW; ++k) tau = fmaxf(tau, taus[k]);
+  const Best top = r0.win;
+  if (p.bad || top.v == kNegInf) {  // nothing to choose from
     if (tid == 0) {
       a.tokens[b] = -1;
       if (a.logprob) a.logprob[b] = __builtin_nanf("");
     }
     return;
   }
-  float z = 0.0f;
-  for (int i = tid; i < a.V; i += kSampleT) z += expf(exponent(no_nan(logit(x, i)), top.v, p.T));
-  z = block_sum(z);
-  int token = top.i;
-  float xt = top.v;
-  if (!p.greedy && p.k > 1) {
-    const bool all = p.k >= a.V && p.top_p >= 1.0f && p.min_p <= 0.0f;
-    float px = kNegInf;   // the pivot: tokens before it are still in the race
-    int pi = 0x7fffffff;
-    for (;;) {  // ends: every round leaves fewer tokens before the pivot, and the first is always kept
-      Best win{-1.0f, 0x7fffffff};
-      int n = 0;
-      float mass = 0.0f;
-      for (int i = tid; i < a.V; i += kSampleT) {
-        const float v = no_nan(logit(x, i));
-        if (v > px || (v == px && i < pi)) {
-          const float wt = expf(exponent(v, top.v, p.T));
-          ++n;
-          mass += wt;
-          if (wt >= p.min_p || i == top.i) win = better(win, Best{wt / fmaxf(r[i], kTiny), i});
+  // Z, and the winner of a race over all tokens
+  Round r1{kNobody, 0, 0.0f};
+  const bool race_all = !p.greedy && !p.filtered;
+  auto join = [&](const Part& q) {
+    if (q.m == kNegInf) return;
+    r1.mass += q.z * weight(q.m, top.v, sc);
+    if (race_all && q.wi != 0x7fffffff) r1.win = better(r1.win, Best{race(weight(q.wx, top.v, sc), q.wr), q.wi, q.wx});
+  };
+  if (tid < nch) join(mine);
+  for (int c = tid + kPickT; c < nch; c += kPickT) join(parts[c]);
+  // the listed tokens that belong to the whole bound
+  float wt[kHeld], v[kHeld];
+  if (choose) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (j0 + k * group >= ln || !(x[k] >= tau)) x[k] = kNegInf;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) v[k] = x[k] > kNegInf ? noise[id[k]] : 1.0f;
+  }
+  r1 = reduce(r1);
+  const float Z = r1.mass;
+  Best token = race_all ? r1.win : top;
+  if (choose) {
+    const float bound = p.top_p * Z;
+    const bool by_p = p.top_p < 1.0f;
+    auto kept = [&](int i, const Round& before) {
+      return i == top.i || (before.n < p.k && (!by_p || before.mass < bound));
+    };
+    bool done = false;
+    if (r0.n == 0) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const bool in = x[k] > kNegInf;
+        wt[k] = in ? weight(x[k], top.v, sc) : 0.0f;
+        v[k] = in && (wt[k] >= p.min_p || id[k] == top.i) ? race(wt[k], v[k]) : -1.0f;
+      }
+      Best pivot = kNobody;  // only tokens before it are still in the race; at first all
+      for (bool all = true;; all = false) {
+        Round r{kNobody, 0, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+          if (x[k] > kNegInf && (all || x[k] > pivot.x || (x[k] == pivot.x && id[k] < pivot.i))) {
+            ++r.n;
+            r.mass += wt[k];
+            r.win = better(r.win, Best{v[k], id[k], x[k]});
+          }
+        }
+        r = reduce(r);
+        if (all) {
+          // the tokens that are not among these stand after all of them, and weigh less than the bound: do they all
+          // fail a filter?
+          const bool within = tau <= -kFltMax || r.n >= p.k || (by_p && r.mass >= bound) ||
+                              (p.min_p > 0.0f && weight(tau, top.v, sc) < p.min_p);
+          if (!within || r.win.v < 0.0f) break;
+        } else if (kept(pivot.i, r)) {
+          done = true;
+          break;
+        }
+        pivot = r.win;
+        if (pivot.i == top.i) {
+          done = true;
+          break;
         }
       }
-      n = block_count(n);
-      mass = block_sum(mass);
-      win = block_best(win);
-      const bool pivot_kept = pi != 0x7fffffff && (pi == top.i || (n < p.k && (p.top_p >= 1.0f || mass < p.top_p * z)));
-      if (pivot_kept) {
-        token = pi;
-        xt = px;
-        break;
+      token = pivot;
+    }
+    if (!done) {
+      // The same over the row. A chunk's winner stands until the pivot comes before it: only such chunks race again.
+      if (tid < nch) stale[tid] = mine.wi == 0x7fffffff;
+      Best champion = kNobody;  // thread c: of chunk c
+      if (tid < nch && mine.wi != 0x7fffffff)
+        champion = Best{race(weight(mine.wx, top.v, sc), mine.wr), mine.wi, mine.wx};
+      Best pivot = kNobody;
+      for (bool all = true;; all = false) {  // ends: fewer tokens race every time, and the first is always kept
+        __syncthreads();
+        for (int c = 0; c < nch; ++c) {
+          if (!stale[c]) continue;
+          Round r{kNobody, 0, 0.0f};
+          for (int v0 = 0; run_start<VE>(v0, c, nch) < a.V; v0 += kPickT * kAhead) {
+            float y[kAhead][VE], q[kAhead][VE];
+            int at[kAhead];
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) at[s] = run_start<VE>(v0 + s * kPickT + tid, c, nch);
+            load_runs<TI, kAhead>(row, a.V, at, y);
+            load_noise<kAhead, VE>(noise, a.V, at, q);
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+              for (int e = 0; e < VE; ++e) {
+                const int i = at[s] + e;
+                if (y[s][e] > kNegInf && (all || y[s][e] > pivot.x || (y[s][e] == pivot.x && i < pivot.i)))
+                  r.win = better(r.win, Best{race(weight(y[s][e], top.v, sc), q[s][e]), i, y[s][e]});
+              }
+            }
+          }
+          r = reduce(r);
+          if (tid == c) champion = r.win;
+        }
+        Round r{champion, 0, 0.0f};
+        pivot = reduce(r).win;
+        if (pivot.i == top.i) break;
+        r = Round{kNobody, 0, 0.0f};
+        constexpr int kBlock = kPickT * VE * kAhead;
+        for (int i0 = 0; i0 < a.V; i0 += kBlock) {
+          float y[kAhead][VE];
+          int at[kAhead];
+#pragma unroll
+          for (int s = 0; s < kAhead; ++s) at[s] = i0 + (s * kPickT + tid) * VE;
+          load_runs<TI, kAhead>(row, a.V, at, y);
+#pragma unroll
+          for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              const bool in = y[s][e] > pivot.x || (y[s][e] == pivot.x && at[s] + e < pivot.i);
+              r.n += in;
+              r.mass += in ? weight_fast(y[s][e], top.v, sc) : 0.0f;
+            }
+          }
+        }
+        r = reduce(r);
+        if (kept(pivot.i, r) && weight(pivot.x, top.v, sc) >= p.min_p) break;
+        if (tid < nch) stale[tid] = champion.i != 0x7fffffff && !(champion.x > pivot.x || (champion.x == pivot.x && champion.i < pivot.i));
       }
-      pi = win.i;
-      px = no_nan(logit(x, pi));
-      if (all || pi == top.i) {
-        token = pi;
-        xt = px;
-        break;
-      }
+      token = pivot;
     }
   }
   if (tid == 0) {
-    a.tokens[b] = token;
-    if (a.logprob) a.logprob[b] = exponent(xt, top.v, p.T) - logf(z);
+    a.tokens[b] = token.i;
+    if (a.logprob) a.logprob[b] = (token.x == top.v ? 0.0f : (token.x - top.v) / p.T) - logf(Z);
   }
+}
+
+// How a batch is cut: chunks of 8192 logits (32 a thread of the scan); 2048 where
+// these would be few, so that more of the chip reads.
+struct Cut {
+  bool fine;
+  int nch, rank, group, cap;
+};
+Cut cut_of(int64_t B, int64_t V) {
+  Cut c;
+  const int64_t big = (V + 8191) / 8192;
+  c.fine = B * big < 256 && V <= 2048 * 256;
+  c.nch = (int)(c.fine ? (V + 2047) / 2048 : big);
+  c.rank = kTarget / (4 * c.nch);
+  c.rank = c.rank < 1 ? 1 : c.rank > 40 ? 40 : c.rank;
+  int pow2 = 1;
+  while (pow2 < c.nch) pow2 *= 2;
+  c.group = kPickT / pow2;
+  c.cap = c.group * kHeld < kListCap ? c.group * kHeld : kListCap;
+  return c;
+}
+
+template <typename TI>
+hipError_t launch_t(const SampleArgs& a, hipStream_t stream) {
+  const Cut c = cut_of(a.B, a.V);
+  Part* parts = (Part*)a.ws;
+  float2* lists = (float2*)(parts + (((int64_t)a.B * c.nch + 7) & ~7LL));
+  const dim3 grid((unsigned)((int64_t)a.B * c.nch));
+  constexpr int full = 32 / Logits<TI>::VE, quarter = 8 / Logits<TI>::VE;
+  if (c.fine)
+    hipLaunchKernelGGL((sample_scan_kernel<TI, quarter>), grid, dim3(kScanT), 0, stream, a, c.nch, c.rank, c.cap, parts, lists);
+  else
+    hipLaunchKernelGGL((sample_scan_kernel<TI, full>), grid, dim3(kScanT), 0, stream, a, c.nch, c.rank, c.cap, parts, lists);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((sample_pick_kernel<TI>), dim3((unsigned)a.B), dim3(kPickT), 0, stream, a, c.nch, c.group, parts, lists);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t sample_workspace_bytes(int64_t B, int64_t V) { return 0; }
+size_t sample_workspace_bytes(int64_t B, int64_t V) {
+  const Cut c = cut_of(B, V);
+  const size_t n = (size_t)B * (size_t)c.nch;
+  return ((n + 7) & ~(size_t)7) * sizeof(Part) + n * kListCap * sizeof(float2);
+}
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream) {
-  if (dtype == 1)
-    hipLaunchKernelGGL((sample_rows_kernel<bf16>), dim3((unsigned)a.B), dim3(kSampleT), 0, stream, a);
-  else
-    hipLaunchKernelGGL((sample_rows_kernel<float>), dim3((unsigned)a.B), dim3(kSampleT), 0, stream, a);
-  return hipGetLastError();
+  return dtype == 1 ? launch_t<bf16>(a, stream) : launch_t<float>(a, stream);
 }
 
 }  // namespace rel
