@@ -15,34 +15,18 @@ namespace {
 // the batch, which every workgroup makes for itself in LDS (8 bytes a request
 // read, no second launch and no pass through memory between them); then a
 // thread finds its token's request by bisection of the ends.
-// Latency-bound: a launch, two dependent reads and the scan.
+// Latency-bound: a launch, two dependent reads (lengths, then page ids) and the
+// scan. Sums are held at kFull, over any bound that they are compared with, so
+// that they stay in 32 bits whatever the counts.
 // ---------------------------------------------------------------------------
-constexpr int kMapT = 1024;
+constexpr int kMapT = 256;
 constexpr int kMapTokens = 4;  // tokens per thread
+constexpr unsigned kFull = (1u << 30) + 1;
 
-struct MapRow {
-  int64_t tokens, have, need;
-  bool valid;
-};
-
-__device__ __forceinline__ MapRow map_row(const PageMapArgs& a, int b) {
-  const int64_t c = a.cached[b], n = a.added[b], p1 = (1 << a.shift) - 1;
-  MapRow r;
-  r.tokens = n > 0 ? n : 0;
-  r.have = c > 0 ? (c + p1) >> a.shift : 0;
-  const int64_t want = (c + n + p1) >> a.shift;
-  r.valid = c >= 0 && n >= 0 && want <= a.W;
-  r.need = r.valid ? want - r.have : 0;
-  return r;
-}
-
-// end and pages: the inclusive sums of tokens and needs at this request
-__device__ __forceinline__ bool map_served(const PageMapArgs& a, const MapRow& r, int end, int pages) {
-  return r.valid && (r.tokens == 0 || end <= a.N) && (r.need == 0 || pages <= a.F);
-}
+__device__ __forceinline__ unsigned add_full(unsigned x, unsigned y) { return min(x + y, kFull); }
 
 // first b in [0, B) with x[b] > v (x ascending); B if none
-__device__ __forceinline__ int first_above(const int* x, int B, int v) {
+__device__ __forceinline__ int first_above(const unsigned* x, int B, unsigned v) {
   int lo = 0, hi = B;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -55,96 +39,116 @@ __device__ __forceinline__ int first_above(const int* x, int B, int v) {
 }
 
 __global__ __launch_bounds__(kMapT) void page_map_kernel(PageMapArgs a) {
-  extern __shared__ int lds[];
-  int* end = lds;           // [B] sums of tokens, held to 2^31 - 1 (N is less)
-  int* pages = lds + a.B;   // [B] sums of needs, held likewise
-  __shared__ int64_t wsum[2][kMapT / 64];
-  __shared__ int total[3];
+  constexpr int NW = kMapT / 64;
+  extern __shared__ unsigned lds[];
+  unsigned* end = lds;           // [B] sums of tokens; before the scan the count itself
+  unsigned* pages = lds + a.B;   // [B] sums of needs
+  int* held = (int*)(lds + 2 * a.B);  // [B] tokens cached, -1 where the request is not served
+  __shared__ unsigned wsum[2][NW];
+  __shared__ int total[3][NW];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int64_t p1 = (1 << a.shift) - 1;
+  const bool first_wg = blockIdx.x == 0;
   const int per = (a.B + kMapT - 1) / kMapT;
   const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-  int64_t t = 0, n = 0;
+  unsigned t = 0, n = 0;
   for (int b = b0; b < b1; ++b) {
-    const MapRow r = map_row(a, b);
-    t += r.tokens;
-    n += r.need;
+    const int64_t c = a.cached[b], add = a.added[b];
+    const int64_t have = (c + p1) >> a.shift, want = (c + add + p1) >> a.shift;
+    const bool valid = c >= 0 && add >= 0 && want <= a.W;
+    end[b] = add > 0 ? min((unsigned)add, kFull) : 0;
+    pages[b] = valid ? (unsigned)(want - have) : 0;
+    held[b] = valid ? (int)c : -1;
+    t = add_full(t, end[b]);
+    n = add_full(n, pages[b]);
   }
-  const int64_t t0 = t, n0 = n;
+  const unsigned t0 = t, n0 = n;
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t tt = __shfl_up(t, o, 64), nn = __shfl_up(n, o, 64);
+    const unsigned tt = __shfl_up(t, o, 64), nn = __shfl_up(n, o, 64);
     if (lane >= o) {
-      t += tt;
-      n += nn;
+      t = add_full(t, tt);
+      n = add_full(n, nn);
     }
   }
   if (lane == 63) {
     wsum[0][w] = t;
     wsum[1][w] = n;
   }
-  if (tid < 3) total[tid] = 0;
+  // the sums before this thread's requests: those of the lane before, and of the waves before
+  t = __shfl_up(t, 1, 64);
+  n = __shfl_up(n, 1, 64);
+  if (lane == 0) t = n = 0;
   __syncthreads();
-  t -= t0;
-  n -= n0;
-  for (int x = 0; x < w; ++x) {
-    t += wsum[0][x];
-    n += wsum[1][x];
-  }
-  for (int b = b0; b < b1; ++b) {
-    const MapRow r = map_row(a, b);
-    t += r.tokens;
-    n += r.need;
-    end[b] = (int)(t < 0x7fffffff ? t : 0x7fffffff);
-    pages[b] = (int)(n < 0x7fffffff ? n : 0x7fffffff);
-  }
-  __syncthreads();
-
-  // the requests' own values: the first workgroup
-  if (blockIdx.x == 0) {
-    int taken = 0, mapped = 0, refused = 0;
-    for (int b = tid; b < a.B; b += kMapT) {
-      const MapRow r = map_row(a, b);
-      const bool s = map_served(a, r, end[b], pages[b]);
-      a.lengths[b] = s ? a.cached[b] + a.added[b] : 0;
-      a.row_start[b + 1] = min(end[b], a.N);
-      if (s) {
-        taken += (int)r.need;
-        mapped += (int)r.tokens;
-      } else {
-        ++refused;
-      }
+#pragma unroll
+  for (int x = 0; x < NW; ++x) {
+    if (x < w) {
+      t = add_full(t, wsum[0][x]);
+      n = add_full(n, wsum[1][x]);
     }
+  }
+  int taken = 0, mapped = 0, refused = 0;
+  for (int b = b0; b < b1; ++b) {
+    const unsigned tokens = end[b], need = pages[b];
+    t = add_full(t, tokens);
+    n = add_full(n, need);
+    const bool served = held[b] >= 0 && (tokens == 0 || t <= (unsigned)a.N) && (need == 0 || n <= (unsigned)a.F);
+    if (first_wg) {
+      a.lengths[b] = served ? held[b] + (int)tokens : 0;
+      a.row_start[b + 1] = (int)min(t, (unsigned)a.N);
+      taken += served ? (int)need : 0;
+      mapped += served ? (int)tokens : 0;
+      refused += !served;
+    }
+    end[b] = t;
+    pages[b] = n;
+    if (!served) held[b] = -1;
+  }
+  if (first_wg) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      taken += __shfl_xor(taken, o, 64);
+      mapped += __shfl_xor(mapped, o, 64);
+      refused += __shfl_xor(refused, o, 64);
+    }
+    if (lane == 0) {
+      total[0][w] = taken;
+      total[1][w] = mapped;
+      total[2][w] = refused;
+    }
+  }
+  __syncthreads();
+  if (first_wg && tid < 3) {
+    int s = 0;
+    for (int x = 0; x < NW; ++x) s += total[tid][x];
+    a.counts[tid] = s;
     if (tid == 0) a.row_start[0] = 0;
-    atomicAdd(&total[0], taken);
-    atomicAdd(&total[1], mapped);
-    atomicAdd(&total[2], refused);
-    __syncthreads();
-    if (tid < 3) a.counts[tid] = total[tid];
   }
 
   // pages taken, in the order of the free list
   const int64_t stride = (int64_t)gridDim.x * kMapT, first = (int64_t)blockIdx.x * kMapT + tid;
-  const int avail = a.B ? min(pages[a.B - 1], a.F) : 0;
+  const int avail = a.B ? (int)min(pages[a.B - 1], (unsigned)a.F) : 0;
   for (int64_t i = first; i < avail; i += stride) {
-    const int b = first_above(pages, a.B, (int)i);
-    const MapRow r = map_row(a, b);
-    if (map_served(a, r, end[b], pages[b]))
-      a.table[(int64_t)b * a.W + r.have + (i - (pages[b] - r.need))] = a.free_pages[i];
+    const int id = a.free_pages[i];
+    const int b = first_above(pages, a.B, (unsigned)i);
+    if (held[b] >= 0) {
+      const int64_t have = (held[b] + p1) >> a.shift;
+      a.table[(int64_t)b * a.W + have + (i - (b ? pages[b - 1] : 0))] = id;
+    }
   }
 
   // tokens
+#pragma unroll 4
   for (int64_t i = first; i < a.N; i += stride) {
     int64_t slot = -1;
     int pos = -1;
-    const int b = first_above(end, a.B, (int)i);
-    if (b < a.B) {
-      const MapRow r = map_row(a, b);
-      if (map_served(a, r, end[b], pages[b])) {
-        pos = (int)(a.cached[b] + (i - (end[b] - r.tokens)));
-        const int j = pos >> a.shift;
-        // a page of this step is read from the free list: its table entry may not be written yet
-        const int64_t id = j < r.have ? a.table[(int64_t)b * a.W + j] : a.free_pages[pages[b] - r.need + (j - r.have)];
-        slot = id * (1 << a.shift) + (pos & ((1 << a.shift) - 1));
-      }
+    const int b = first_above(end, a.B, (unsigned)i);
+    if (b < a.B && held[b] >= 0) {
+      pos = held[b] + (int)(i - (b ? end[b - 1] : 0));
+      const int j = pos >> a.shift, have = (int)((held[b] + p1) >> a.shift);
+      // a page of this step is read from the free list: its table entry may not be written yet
+      const int64_t id = j < have ? a.table[(int64_t)b * a.W + j] : a.free_pages[(b ? pages[b - 1] : 0) + (unsigned)(j - have)];
+      slot = id * (1 << a.shift) + (pos & (int)p1);
     }
     a.slots[i] = slot;
     a.positions[i] = pos;
@@ -314,7 +318,7 @@ hipError_t append_t(const AppendArgs& a, hipStream_t stream) {
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
   const int64_t want = ((int64_t)a.N + kMapT * kMapTokens - 1) / (kMapT * kMapTokens);
   const unsigned grid = (unsigned)(want < 1 ? 1 : want > 2048 ? 2048 : want);
-  hipLaunchKernelGGL(page_map_kernel, dim3(grid), dim3(kMapT), (size_t)a.B * 8, stream, a);
+  hipLaunchKernelGGL(page_map_kernel, dim3(grid), dim3(kMapT), (size_t)a.B * 12, stream, a);
   return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@ struct PagedCache {
   int H, D;
 };
 
-// The largest batch of a page map: its scan lives in LDS, 8 bytes a request.
+// The largest batch of a page map: its scan lives in LDS, 12 bytes a request.
 constexpr int kMapMaxB = 4096;
 
 struct PageMapArgs {
