@@ -20,7 +20,6 @@ namespace {
 // that they stay in 32 bits whatever the counts.
 // ---------------------------------------------------------------------------
 constexpr int kMapT = 256;
-constexpr int kMapTokens = 4;  // tokens per thread
 constexpr unsigned kFull = (1u << 30) + 1;
 
 __device__ __forceinline__ unsigned add_full(unsigned x, unsigned y) { return min(x + y, kFull); }
@@ -316,7 +315,8 @@ hipError_t append_t(const AppendArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
-  const int64_t want = ((int64_t)a.N + kMapT * kMapTokens - 1) / (kMapT * kMapTokens);
+  // a token per thread: 64 requests and 69 tokens 4.1 us, 96 and 66000 4.9 (8.4 with four tokens a thread)
+  const int64_t want = ((int64_t)a.N + kMapT - 1) / kMapT;
   const unsigned grid = (unsigned)(want < 1 ? 1 : want > 2048 ? 2048 : want);
   hipLaunchKernelGGL(page_map_kernel, dim3(grid), dim3(kMapT), (size_t)a.B * 12, stream, a);
   return hipGetLastError();
