@@ -3,13 +3,18 @@
 // the request's block table (eq. 2 at position i = the request's length).
 //
 // The mathematics is that of decode.hip: the history is split into slices, each
-// leaves its Exchange scan state (m, l, z) of eq. (11), and the states of a row
-// are joined with Self and the count correction (eqs. 12-13). One workgroup
-// reads a slice of one key head for up to GQ of the query heads that share it,
-// so that shared keys are read once. The slice's block-table entries are turned
-// into element offsets in LDS first; a key's row is then one LDS read away. A
-// batch whose rows have one slice each is finished by the same launch.
+// leaves its Exchange scan state (m, l, z) of eq. (11), here with m in units of
+// ln 2, and the states of a row are joined with Self and the count correction
+// (eqs. 12-13). One workgroup reads a slice of one key head for the query heads
+// that share it, so that shared keys are read once. The slice's block-table
+// entries are turned into element offsets in LDS first; a key's row is then one
+// LDS read away. A batch whose rows have one slice each is finished by the same
+// launch.
 //
+// Two states kernels. In bf16 the products run on the matrix cores, also where
+// a key head has one query: sixteen query columns cost what one does, and a wave
+// then spends no vector instruction on products and no lane moves on sums. In
+// fp32 lanes share a key and multiply themselves.
 // Bound by the reads of K and V.
 #include "kernels.h"
 #include "lanes.h"
@@ -20,23 +25,10 @@ namespace rel {
 namespace {
 
 constexpr int kMergeT = 256;
+constexpr int kFewGroups = 512;  // workgroups (two per CU) below which they get more waves
 constexpr int kUnroll = 2;  // keys per lane group whose loads are in flight together
 
-template <typename TI, int VEC>
-struct Row;
-template <>
-struct Row<bf16, 8> {
-  static __device__ __forceinline__ void load(const bf16* p, float (&x)[8]) {
-    const uintx4 u = *reinterpret_cast<const uintx4*>(p);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      x[2 * t] = bf16_lo(u[t]);
-      x[2 * t + 1] = bf16_hi(u[t]);
-    }
-  }
-};
-template <>
-struct Row<float, 4> {
+struct Row {
   static __device__ __forceinline__ void load(const float* p, float (&x)[4]) {
     const float4 u = *reinterpret_cast<const float4*>(p);
     x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
@@ -56,8 +48,8 @@ template <int VEC>
 __device__ __forceinline__ void merge_into(float& m, float& l, float (&z)[VEC], float mo, float lo,
                                            const float (&zo)[VEC]) {
   const float mn = fmaxf(m, mo);
-  const float a = m == kNegInf ? 0.0f : fast_exp2((m - mn) * kLog2e);
-  const float b = mo == kNegInf ? 0.0f : fast_exp2((mo - mn) * kLog2e);
+  const float a = m == kNegInf ? 0.0f : fast_exp2(m - mn);
+  const float b = mo == kNegInf ? 0.0f : fast_exp2(mo - mn);
   l = l * a + lo * b;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) z[e] = z[e] * a + zo[e] * b;
@@ -108,7 +100,7 @@ __device__ __forceinline__ void finish_row(const PagedDecodeArgs& a, int b, int 
   const float lam = *a.lambda;
   float g = 0.0f, omg = 1.0f, zr0 = 0.0f, zr1 = 0.0f, lnZ = S;
   if (!(l == 0.0f)) {                               // some history (or a NaN in it)
-    const float A = m + logf(l) - lam * ln_i;       // A_i = L^E_i - lambda ln i (eq. 5)
+    const float A = m * kLn2 + logf(l) - lam * ln_i;       // A_i = L^E_i - lambda ln i (eq. 5)
     g = 1.0f / (1.0f + expf(S - A));                // g = sigmoid(A - S)
     omg = 1.0f / (1.0f + expf(A - S));              // 1 - g = sigmoid(S - A)
     const float il = 1.0f / l;
@@ -124,13 +116,56 @@ __device__ __forceinline__ void finish_row(const PagedDecodeArgs& a, int b, int 
   if (lane == 0 && a.row_stat) a.row_stat[(int64_t)b * a.Hq + hq] = s.ok ? lnZ + lam * ln_i : nan;
 }
 
+// Offsets of the slice's pages p0 .. p1 (of head h) into LDS, by all NT threads; whether the thread met a bad page.
+template <int NT>
+__device__ __forceinline__ int page_offsets(const PagedDecodeArgs& a, int b, int h, int p0, int p1, int64_t* offs) {
+  int bad = 0;
+  for (int p = p0 + threadIdx.x; p <= p1; p += NT) {
+    const int id = a.table[(int64_t)b * a.W + p];
+    const bool ok = id >= 0 && id < a.c.num_pages;
+    offs[p - p0] = (int64_t)(ok ? id : 0) * a.c.sp + (int64_t)h * a.c.sh;
+    bad |= !ok;
+  }
+  return bad;
+}
+
+// One wave joins the NW waves' states of a row, (m, l, z) at st + wave * stride in
+// LDS, in the waves' order, and stores the slice's state or finishes the row.
+template <typename TI, int NW>
+__device__ __forceinline__ void join_waves(const PagedDecodeArgs& a, int slice, int b, int hq, int len, int lane,
+                                           const float* st, int stride) {
+  const int D = a.c.D;
+  SelfEntry self;
+  if (a.nsplit == 1) self = read_self<TI>(a, b, hq, len, lane);
+  float m = kNegInf, l = 0.0f, z[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int x = 0; x < NW; ++x) {
+    const float* s = st + x * stride;
+    const float zo[2] = {lane < D ? s[2 + lane] : 0.0f, lane + 64 < D ? s[2 + 64 + lane] : 0.0f};
+    merge_into<2>(m, l, z, s[0], s[1], zo);
+  }
+  if (a.nsplit == 1) {
+    finish_row<TI>(a, b, hq, len, lane, self, m, l, z[0], z[1]);
+    return;
+  }
+  float* out = a.states + ((int64_t)slice * a.B * a.Hq + (int64_t)b * a.Hq + hq) * (D + 2);
+  if (lane == 0) {
+    out[0] = m;
+    out[1] = l;
+  }
+  if (lane < D) out[2 + lane] = z[0];
+  if (lane + 64 < D) out[2 + 64 + lane] = z[1];
+}
+
 // Exchange states of one slice for the query heads [r GQ, r GQ + GQ) of one key
 // head (workgroup = (request, key head, r, slice)). LPK lanes share a key: lane
 // c of the group holds VEC channels (16 bytes) of the queries and reads those
 // of the key and value rows; every lane group keeps its own running (m, l, z),
 // and the groups of the workgroup meet in LDS in a fixed order.
-template <typename TI, int VEC, int LPK, int GQ, int NT>
-__global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
+template <int LPK, int GQ, int NT>
+__global__ __launch_bounds__(NT) void paged_states_f32_kernel(PagedDecodeArgs a) {
+  typedef float TI;
+  constexpr int VEC = 4;
   constexpr int KPW = 64 / LPK;  // keys per wave and step
   constexpr int NW = NT / 64;
   static_assert(NW >= GQ, "a wave for each query head at the end");
@@ -148,6 +183,7 @@ __global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
   const int len = length_of(a, b);
   const int s0 = slice * a.slice, s1 = min(s0 + a.slice, len - 1);  // Exchange keys only: j < i - 1 (zero-based)
   const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
+  if (s1 <= s0 && a.nsplit > 1) return;  // a slice past the request's end: nobody reads its state
 
   float m[GQ], l[GQ], z[GQ][VEC];
 #pragma unroll
@@ -158,19 +194,13 @@ __global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
     for (int e = 0; e < VEC; ++e) z[g][e] = 0.0f;
   }
   if (s1 > s0) {  // uniform in the workgroup
-    int bad = 0;
-    for (int p = p0 + threadIdx.x; p <= (s1 - 1) >> a.c.shift; p += NT) {
-      const int id = a.table[(int64_t)b * a.W + p];
-      const bool ok = id >= 0 && id < a.c.num_pages;
-      offs[p - p0] = (int64_t)(ok ? id : 0) * a.c.sp + (int64_t)h * a.c.sh;
-      bad |= !ok;
-    }
+    int bad = page_offsets<NT>(a, b, h, p0, (s1 - 1) >> a.c.shift, offs);
     float q[GQ][VEC];
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) q[g][e] = 0.0f;
-      if (chan && g < ng) Row<TI, VEC>::load((const TI*)a.q + ((int64_t)b * a.Hq + hq0 + g) * a.c.D + c0, q[g]);
+      if (chan && g < ng) Row::load((const TI*)a.q + ((int64_t)b * a.Hq + hq0 + g) * a.c.D + c0, q[g]);
     }
     bad = __syncthreads_or(bad);
     const TI *K = (const TI*)a.k + c0, *V = (const TI*)a.v + c0;
@@ -187,8 +217,8 @@ __global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
         for (int e = 0; e < VEC; ++e) kx[u][e] = vx[u][e] = 0.0f;
         if (ok[u] && chan) {
           const int64_t off = offs[(j >> a.c.shift) - p0] + (int64_t)((j & mask) * a.c.st);
-          Row<TI, VEC>::load(K + off, kx[u]);
-          Row<TI, VEC>::load(V + off, vx[u]);
+          Row::load(K + off, kx[u]);
+          Row::load(V + off, vx[u]);
         }
       }
 #pragma unroll
@@ -201,10 +231,10 @@ __global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
           d = lane_group_sum<LPK>(d);
           if (ok[u]) {
             const float uu = d * a.scale;
-            const float E = uu * sigm(uu);  // Exchange map, eq. (2)
+            const float E = uu * sigm(uu) * kLog2e;  // Exchange map, eq. (2)
             const float mn = fmaxf(m[g], E);
-            const float cr = m[g] == kNegInf ? 0.0f : fast_exp2((m[g] - mn) * kLog2e);
-            const float p = fast_exp2((E - mn) * kLog2e);
+            const float cr = m[g] == kNegInf ? 0.0f : fast_exp2(m[g] - mn);
+            const float p = fast_exp2(E - mn);
             l[g] = l[g] * cr + p;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) z[g][e] = __builtin_fmaf(p, vx[u][e], z[g][e] * cr);
@@ -244,27 +274,192 @@ __global__ __launch_bounds__(NT) void paged_states_kernel(PagedDecodeArgs a) {
     }
   }
   __syncthreads();
-  // wave g joins the waves' states of query head g: lane holds channels lane and lane + 64
-  if (w >= ng) return;
-  const int hq = hq0 + w;
-  SelfEntry self;
-  if (a.nsplit == 1) self = read_self<TI>(a, b, hq, len, lane);
-  float mm = kNegInf, ll = 0.0f, zz[2] = {0.0f, 0.0f};
-  for (int x = 0; x < NW; ++x) {
-    const float zo[2] = {lane < a.c.D ? red[x][w][2 + lane] : 0.0f, lane + 64 < a.c.D ? red[x][w][2 + 64 + lane] : 0.0f};
-    merge_into<2>(mm, ll, zz, red[x][w][0], red[x][w][1], zo);
+  // wave g joins the waves' states of query head g
+  if (w < ng) join_waves<TI, NW>(a, slice, b, hq0 + w, len, lane, &red[0][w][0], GQ * (2 + 128));
+}
+
+// The same in bf16 on the matrix cores, for up to 16 query heads of a key head
+// (workgroup = (request, key head, group of 16, slice)). A wave takes 32 keys at a
+// time, two tiles of 16, DB blocks of 16 channels. Rows are read whole, neighbouring
+// lanes neighbouring chunks of 16 bytes, and go through LDS (the wave's own, no
+// barrier) into operands:
+//   U^T = K q^T (16 x 16 x 32): lane (g, r) = (lane / 16, lane % 16) holds chunks g,
+//     g + 4, ... of key r and of query r, and gets the evidence of keys 4 g .. 4 g + 3
+//     for query r.
+//   z^T += V^T P (16 x 16 x 32): P needs the lane's own eight values in place, the
+//     contraction running over keys 4 g .. 4 g + 3 of both tiles; V comes back from LDS
+//     by transpose reads.
+// z of query r stays in lanes r, r + 16, ..., where its maximum is, so a new maximum
+// rescales in place; that is rare after the first keys and costs a branch else.
+// P is split as hi + lo, two bf16 numbers of 16 significant bits together: the
+// matrix cores have the time, and z keeps fp32-like accuracy.
+// Measured, 64 requests of 1024 to 4096 tokens, 12 heads x 64 (504 MB): 99 us, 5.1
+// TB/s; 2 x 16 x 128 of up to 65536 (1.02 GB): 181 us, 5.6 TB/s. With each lane
+// reading its operand of K from memory (64 bytes of a row per load) 123 and 188;
+// with the slices of a row together rather than the heads of a slice 107 of the
+// 123; with the vector unit's products (four query heads a pass) 99 and 184 at the
+// same slices, but 135 against 73 for four query heads a key head (295 MB).
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ floatx4_t mfma16(const bf16x8& x, const bf16x8& y, const floatx4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+}
+__device__ __forceinline__ bf16x8 pack8(const float (&x)[8]) {
+  bf16x8 o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = (bf16)x[e];
+  return o;
+}
+
+template <int DB, int NW>
+__global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeArgs a) {
+  constexpr int KS = (DB + 1) / 2;        // products of 32 channels
+  constexpr int ROWB = DB * 32 + 32;      // bytes of a V row in LDS: 32 more, so that rows fall on other banks
+  constexpr int WAVEB = 32 * ROWB > 16 * (2 + 16 * DB) * 4 ? 32 * ROWB : 16 * (2 + 16 * DB) * 4;
+  static_assert(WAVEB % 16 == 0, "16-byte rows");
+  __shared__ __align__(16) unsigned char vlds[NW][WAVEB];
+  extern __shared__ int64_t offs[];       // the slice's pages: element offset of (page, head)
+  const int nr = (a.G + 15) / 16;
+  const int rows = gridDim.x / a.nsplit;  // heads of a request stand together in the pages: they run together
+  const int slice = blockIdx.x / rows;
+  const int row = blockIdx.x % rows;      // (b, h, group)
+  const int grp = row % nr, h = row / nr % a.c.H, b = row / nr / a.c.H;
+  const int hq0 = h * a.G + grp * 16, ng = min(16, a.G - grp * 16);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int g = lane >> 4, r = lane & 15;
+  const int len = length_of(a, b);
+  const int s0 = slice * a.slice, s1 = min(s0 + a.slice, len - 1);  // Exchange keys only: j < i - 1 (zero-based)
+  const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
+  if (s1 <= s0 && a.nsplit > 1) return;   // a slice past the request's end: nobody reads its state
+
+  float m = kNegInf, l = 0.0f;
+  floatx4_t z[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) z[d] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  if (s1 > s0) {  // uniform in the workgroup
+    int bad = page_offsets<NW * 64>(a, b, h, p0, (s1 - 1) >> a.c.shift, offs);
+    const uintx4 none = {0, 0, 0, 0};
+    bf16x8 q[KS];
+    bool chan[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c0 = (4 * s + g) * 8;
+      chan[s] = c0 < a.c.D;
+      uintx4 u = none;
+      if (chan[s] && r < ng) u = *reinterpret_cast<const uintx4*>((const bf16*)a.q + ((int64_t)b * a.Hq + hq0 + r) * a.c.D + c0);
+      q[s] = __builtin_bit_cast(bf16x8, u);
+    }
+    // 16-byte chunk x of the tile's 32 rows is row x / nch, chunk x % nch: lane and load i take chunk 64 i + lane
+    const int nch = a.c.D / 8, nld = (nch + 1) / 2;
+    int krow[DB], kcol[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      const int x = min(64 * i + lane, 32 * nch - 1);
+      krow[i] = x / nch;
+      kcol[i] = x - krow[i] * nch;
+    }
+    bad = __syncthreads_or(bad);
+    const bf16 *K = (const bf16*)a.k, *V = (const bf16*)a.v;
+    const unsigned char* kr = vlds[w] + r * ROWB + g * 16;                        // this lane's operand chunks of K
+    const unsigned char* vr = vlds[w] + (4 * g + (r >> 2)) * ROWB + (r & 3) * 8;  // where its transpose reads start
+    uintx4 kx[DB], vx[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) kx[i] = vx[i] = none;
+    auto load = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        if (i < nld) {
+          const int j = min(base + krow[i], s1 - 1);  // past the end: the last key again, which counts for nothing
+          const int64_t off = offs[(j >> a.c.shift) - p0] + (int64_t)((j & mask) * a.c.st + kcol[i] * 8);
+          kx[i] = *reinterpret_cast<const uintx4*>(K + off);
+          vx[i] = *reinterpret_cast<const uintx4*>(V + off);
+        }
+      }
+    };
+    if (s0 + 32 * w < s1) load(s0 + 32 * w);
+    for (int base = s0 + 32 * w; base < s1; base += 32 * NW) {
+      // K through LDS into operands, then V into the same place: a wave's LDS accesses keep their order
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+        if (i < nld) *reinterpret_cast<uintx4*>(vlds[w] + krow[i] * ROWB + kcol[i] * 16) = kx[i];
+      floatx4_t u[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        u[t] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          uintx4 x = none;
+          if (chan[s]) x = *reinterpret_cast<const uintx4*>(kr + 16 * t * ROWB + 64 * s);
+          u[t] = mfma16(__builtin_bit_cast(bf16x8, x), q[s], u[t]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+        if (i < nld) *reinterpret_cast<uintx4*>(vlds[w] + krow[i] * ROWB + kcol[i] * 16) = vx[i];
+      // the registers are free: the next keys' loads run beside the rest of this step
+      if (base + 32 * NW < s1) load(base + 32 * NW);
+      float e[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float uu = u[t][x] * a.scale;
+          const float E = uu * sigm(uu) * kLog2e;  // Exchange map, eq. (2)
+          e[4 * t + x] = base + 16 * t + 4 * g + x < s1 ? E : kNegInf;
+        }
+      }
+      float top = e[0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) top = fmaxf(top, e[x]);
+      if (__any(top > m)) {  // a new maximum of some query
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m, top), cr = m == kNegInf ? 0.0f : fast_exp2(m - mn);
+        l *= cr;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) z[d] *= cr;
+        m = mn;
+      }
+      float lo[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        e[x] = fast_exp2(e[x] - m);
+        l += e[x];
+      }
+      const bf16x8 ph = pack8(e);
+      const uintx4 pu = __builtin_bit_cast(uintx4, ph);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        lo[2 * x] = e[2 * x] - bf16_lo(pu[x]);
+        lo[2 * x + 1] = e[2 * x + 1] - bf16_hi(pu[x]);
+      }
+      const bf16x8 pl = pack8(lo);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const bf16x8 vt = tr_operand(vr + 32 * d, vr + 16 * ROWB + 32 * d);
+        z[d] = mfma16(vt, ph, z[d]);
+        z[d] = mfma16(vt, pl, z[d]);
+      }
+    }
+    if (bad) l = __builtin_nanf("");
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
   }
-  if (a.nsplit == 1) {
-    finish_row<TI>(a, b, hq, len, lane, self, mm, ll, zz[0], zz[1]);
-    return;
+  // the wave's state of query r into its LDS: m, l, z
+  constexpr int SW = 2 + 16 * DB;
+  float* st = reinterpret_cast<float*>(vlds[w]);
+  if (r < ng) {
+    if (g == 0) {
+      st[r * SW] = m;
+      st[r * SW + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) st[r * SW + 2 + 16 * d + 4 * g + x] = z[d][x];
   }
-  float* st = a.states + ((int64_t)slice * a.B * a.Hq + (int64_t)b * a.Hq + hq) * (a.c.D + 2);
-  if (lane == 0) {
-    st[0] = mm;
-    st[1] = ll;
-  }
-  if (lane < a.c.D) st[2 + lane] = zz[0];
-  if (lane + 64 < a.c.D) st[2 + 64 + lane] = zz[1];
+  __syncthreads();
+  for (int y = w; y < ng; y += NW)
+    join_waves<bf16, NW>(a, slice, b, hq0 + y, len, lane, reinterpret_cast<const float*>(vlds[0]) + y * SW, WAVEB / 4);
 }
 
 // One workgroup per (b, query head): joins the row's states. Only the slices
@@ -321,37 +516,37 @@ __global__ __launch_bounds__(kMergeT) void paged_merge_kernel(PagedDecodeArgs a)
   finish_row<TI>(a, b, hq, len, lane, self, m, l, z[0], z[1]);
 }
 
-template <typename TI, int VEC, int LPK, int GQ>
-void launch_states(const PagedDecodeArgs& a, hipStream_t stream) {
+// Bytes of LDS for the offsets of a slice's pages.
+size_t offsets_bytes(const PagedDecodeArgs& a) { return (size_t)((a.slice >> a.c.shift) + 2) * sizeof(int64_t); }
+
+template <int LPK, int GQ>
+void launch_f32(const PagedDecodeArgs& a, hipStream_t stream) {
   constexpr int NT = 256;
-  const int nr = (a.G + GQ - 1) / GQ;
-  const size_t lds = (size_t)((a.slice >> a.c.shift) + 2) * sizeof(int64_t);
-  hipLaunchKernelGGL((paged_states_kernel<TI, VEC, LPK, GQ, NT>), dim3((unsigned)((int64_t)a.nsplit * a.B * a.c.H * nr)),
-                     dim3(NT), lds, stream, a);
+  const int64_t grid = (int64_t)a.nsplit * a.B * a.c.H * ((a.G + GQ - 1) / GQ);
+  hipLaunchKernelGGL((paged_states_f32_kernel<LPK, GQ, NT>), dim3((unsigned)grid), dim3(NT), offsets_bytes(a), stream, a);
 }
-
-template <typename TI, int VEC, int LPK>
-void launch_states_g(const PagedDecodeArgs& a, hipStream_t stream) {
+template <int LPK>
+void launch_f32_g(const PagedDecodeArgs& a, hipStream_t stream) {
   if (a.G == 1)
-    launch_states<TI, VEC, LPK, 1>(a, stream);
+    launch_f32<LPK, 1>(a, stream);
   else if (a.G == 2)
-    launch_states<TI, VEC, LPK, 2>(a, stream);
+    launch_f32<LPK, 2>(a, stream);
   else
-    launch_states<TI, VEC, LPK, 4>(a, stream);
+    launch_f32<LPK, 4>(a, stream);
 }
 
-template <typename TI, int VEC>
-hipError_t launch_t(const PagedDecodeArgs& a, hipStream_t stream) {
-  const int lanes = (a.c.D + VEC - 1) / VEC;
-  if (lanes <= 4)
-    launch_states_g<TI, VEC, 4>(a, stream);
-  else if (lanes <= 8)
-    launch_states_g<TI, VEC, 8>(a, stream);
-  else if (lanes <= 16)
-    launch_states_g<TI, VEC, 16>(a, stream);
+template <int DB>
+void launch_bf16(const PagedDecodeArgs& a, hipStream_t stream) {
+  const int64_t grid = (int64_t)a.nsplit * a.B * a.c.H * ((a.G + 15) / 16);
+  if (grid < kFewGroups)
+    hipLaunchKernelGGL((paged_states_bf16_kernel<DB, 8>), dim3((unsigned)grid), dim3(512), offsets_bytes(a), stream, a);
   else
-    launch_states_g<TI, VEC, 32>(a, stream);
-  hipError_t e = hipGetLastError();
+    hipLaunchKernelGGL((paged_states_bf16_kernel<DB, 4>), dim3((unsigned)grid), dim3(256), offsets_bytes(a), stream, a);
+}
+
+template <typename TI>
+hipError_t launch_merge(const PagedDecodeArgs& a, hipStream_t stream) {
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   const dim3 grid((unsigned)((int64_t)a.B * a.Hq));
   if (a.c.D <= 64)
@@ -363,14 +558,41 @@ hipError_t launch_t(const PagedDecodeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Slices of the history: about kTargetGroups workgroups, of at least kMinSlice
+// keys; a history of up to kOneSlice is not split, and its rows need no second
+// launch.
 void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int* slice, int* nsplit) {
-  const int64_t hist = max_len > 1 ? max_len - 1 : 1;
-  *slice = 256;
-  *nsplit = (int)((hist + *slice - 1) / *slice);
+  constexpr int64_t kTargetGroups = 1536, kMinSlice = 128, kMaxSlice = 4096, kOneSlice = 256;
+  const int64_t hist = max_len > 1 ? max_len - 1 : 1, rows = B * H * ((G + 15) / 16);
+  int64_t s = kMinSlice;
+  while (s < kMaxSlice && s * kTargetGroups < hist * rows) s *= 2;
+  if (hist <= kOneSlice) s = kOneSlice;
+  *slice = (int)s;
+  *nsplit = (int)((hist + s - 1) / s);
 }
 
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, hipStream_t stream) {
-  return dtype == 1 ? launch_t<bf16, 8>(a, stream) : launch_t<float, 4>(a, stream);
+  const int D = a.c.D;
+  if (dtype == 1) {
+    if (D <= 32)
+      launch_bf16<2>(a, stream);
+    else if (D <= 64)
+      launch_bf16<4>(a, stream);
+    else if (D <= 96)
+      launch_bf16<6>(a, stream);
+    else
+      launch_bf16<8>(a, stream);
+    return launch_merge<bf16>(a, stream);
+  }
+  if (D <= 16)
+    launch_f32_g<4>(a, stream);
+  else if (D <= 32)
+    launch_f32_g<8>(a, stream);
+  else if (D <= 64)
+    launch_f32_g<16>(a, stream);
+  else
+    launch_f32_g<32>(a, stream);
+  return launch_merge<float>(a, stream);
 }
 
 }  // namespace rel
