@@ -645,43 +645,45 @@ def relation_linear_gated_bwd(p1, p2, v, r, a_log, dt_bias, dout, *, rope_dim: i
 # ---------------------------------------------------------------------------
 # Serving from a paged cache
 # ---------------------------------------------------------------------------
-def _on_gpu(**tensors):
-    """The device that all the given tensors (None apart) share."""
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise ValueError(f"{name} must be a tensor on the GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, other tensors on {dev}")
+def _on_gpu(first, *rest) -> int:
+    """The index of the GPU that all the given tensors (None apart) are on. A step of a serving loop is a few calls
+    of microseconds: the checks of these functions are kept to one look at each tensor."""
+    dev = first.get_device() if isinstance(first, torch.Tensor) else -1
+    if dev < 0:
+        raise ValueError("the tensors must be on the GPU")
+    for t in rest:
+        if t is not None and (not isinstance(t, torch.Tensor) or t.get_device() != dev):
+            raise ValueError("all tensors must be on the GPU of the first")
     return dev
 
 
-def _out(out, name, shape, dtype, dev):
-    """out[name] where the caller gives it (checked), or a new tensor."""
+def _given(out, name, shape, dtype, dev):
+    """out[name] where the caller gives it (checked), or None."""
     t = None if out is None else out.get(name)
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    if t.shape != torch.Size(shape) or t.dtype != dtype or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    if t is not None and (t.shape != torch.Size(shape) or t.dtype != dtype or t.get_device() != dev or
+                          not t.is_contiguous()):
+        raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {dev}")
     return t
+
+
+def _ready(t: torch.Tensor, dtype) -> torch.Tensor:
+    """``t`` in ``dtype``, contiguous: itself where it is."""
+    return t if t.dtype == dtype and t.is_contiguous() else t.detach().to(dtype).contiguous()
 
 
 def make_pages(k_cache: torch.Tensor, v_cache: torch.Tensor) -> RelPages:
     """The pools [num_pages, H, page_size, D], with any strides that the library takes."""
-    if k_cache.dim() != 4:
+    shape, strides, dt = k_cache.shape, k_cache.stride(), k_cache.dtype
+    if len(shape) != 4:
         raise ValueError("caches must be [num_pages, H, page_size, D]")
-    shape, strides = k_cache.shape, k_cache.stride()
-    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype != k_cache.dtype:
+    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype != dt:
         raise ValueError("k_cache and v_cache must share shape, strides and dtype")
-    if strides[3] != 1 and shape[3] != 1:
-        raise ValueError("the last dimension must be contiguous")
     P, H, page, D = shape
-    sp, sh, st = (s if n > 1 else 0 for s, n in zip(strides, shape[:3]))  # a stride over one entry says nothing
-    return RelPages(P, page, H, D, _dtype_code(k_cache.dtype), sp, sh, st)
+    sp, sh, st, sd = strides
+    if sd != 1 and D != 1:
+        raise ValueError("the last dimension must be contiguous")
+    # a stride over one entry says nothing
+    return RelPages(P, page, H, D, _dtype_code(dt), sp if P > 1 else 0, sh if H > 1 else 0, st if page > 1 else 0)
 
 
 def relation_page_map(cached, added, table, free_pages, page_size: int, max_tokens: int, *, out=None):
@@ -690,24 +692,31 @@ def relation_page_map(cached, added, table, free_pages, page_size: int, max_toke
     row_start [B + 1], slots int64 [max_tokens], positions [max_tokens], counts [3]: pages taken, tokens mapped,
     requests not served), in the tensors of ``out`` where given."""
     lib = load_library()
-    dev = _on_gpu(cached=cached, added=added, table=table, free_pages=free_pages)
-    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+    i32 = torch.int32
+    dev = _on_gpu(table, cached, added, free_pages)
+    if table.dim() != 2 or table.dtype != i32 or not table.is_contiguous():
         raise ValueError("table must be a contiguous int32 [B, W] tensor")
     B, W = table.shape
     if cached.shape != (B,) or added.shape != (B,) or free_pages.dim() != 1:
         raise ValueError("cached and added must be [B], free_pages [F]")
-    cached, added = _dense(cached, dev, torch.int32), _dense(added, dev, torch.int32)
-    free_pages = _dense(free_pages, dev, torch.int32)
-    i32, N = torch.int32, int(max_tokens)
+    cached, added, free_pages = _ready(cached, i32), _ready(added, i32), _ready(free_pages, i32)
+    N = int(max_tokens)
     if N < 0:
         raise ValueError("max_tokens must not be negative")
-    lengths, row_start = _out(out, "lengths", (B,), i32, dev), _out(out, "row_start", (B + 1,), i32, dev)
-    slots, positions = _out(out, "slots", (N,), torch.int64, dev), _out(out, "positions", (N,), i32, dev)
-    counts = _out(out, "counts", (3,), i32, dev)
+    if out is None:  # one allocation for the int32 outputs
+        lengths, row_start, positions, counts = table.new_empty(2 * B + N + 4).split_with_sizes((B, B + 1, N, 3))
+        slots = table.new_empty(N, dtype=torch.int64)
+    else:
+        new = lambda name, n, dt: _given(out, name, (n,), dt, dev) if out.get(name) is not None else \
+            table.new_empty(n, dtype=dt)
+        lengths, row_start, positions = new("lengths", B, i32), new("row_start", B + 1, i32), new("positions", N, i32)
+        counts, slots = new("counts", 3, i32), new("slots", N, torch.int64)
     m = RelPageMap(B, W, int(page_size), N, free_pages.shape[0])
-    st = lib.relation_page_map(ctypes.byref(m), _ptr(cached), _ptr(added), _ptr(free_pages), _ptr(table),
-                               _ptr(lengths), _ptr(row_start), _ptr(slots), _ptr(positions), _ptr(counts), _stream())
-    _check(st, "relation_page_map")
+    st = lib.relation_page_map(ctypes.byref(m), cached.data_ptr(), added.data_ptr(), free_pages.data_ptr(),
+                               table.data_ptr(), lengths.data_ptr(), row_start.data_ptr(), slots.data_ptr(),
+                               positions.data_ptr(), counts.data_ptr(), _stream())
+    if st:
+        _check(st, "relation_page_map")
     return {"table": table, "lengths": lengths, "row_start": row_start, "slots": slots, "positions": positions,
             "counts": counts}
 
@@ -722,34 +731,43 @@ def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, t
     slots (int64 [N]) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc. With q [N, Hq, D], returns
     the rotated and padded queries [N, Hq, Dc] (out["q"] where given), else None. rope_base 0 or None: no RoPE."""
     lib = load_library()
-    dev = _on_gpu(k=k, v=v, k_cache=k_cache, v_cache=v_cache, slots=slots, positions=positions, q=q)
+    dev = _on_gpu(k, v, k_cache, v_cache, slots, positions, q)
     c = make_pages(k_cache, v_cache)
-    if pairing not in REL_GIVENS:
+    givens = REL_GIVENS.get(pairing)
+    if givens is None:
         raise ValueError("pairing must be None, 'A' or 'B'")
     if k.dim() != 3 or k.shape[1] != c.H or k.dtype != k_cache.dtype:
         raise ValueError("k and v must be [N, H, D] with the caches' heads and dtype")
     N, H, D = k.shape
     k = _rows(k)
-    (v,) = _same_layout(k, v)
+    ks = k.stride()
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("v must be as k")
+    if v.stride() != ks:
+        v = _same_layout(k, v)[0]
     if slots.shape != (N,) or positions.shape != (N,):
         raise ValueError("slots and positions must be [N]")
-    slots, positions = _dense(slots, dev, torch.int64), _dense(positions, dev, torch.int32)
-    th = _theta_tensor(theta, H, dev)
-    if pairing is not None and th is None:
+    slots, positions = _ready(slots, torch.int64), _ready(positions, torch.int32)
+    th = None if theta is None else _theta_tensor(theta, H, k.device)
+    if givens and th is None:
         raise ValueError("theta is required for Givens mixing")
-    Hq = 0
-    q_out, qs = None, (0, 0)
+    Hq = qt = qh = 0
+    q_out = None
     if q is not None:
         if q.dim() != 3 or q.shape[0] != N or q.shape[2] != D or q.dtype != k.dtype:
             raise ValueError("q must be [N, Hq, D] with k's dtype")
         q = _rows(q)
-        Hq, qs = q.shape[1], q.stride()
-        q_out = _out(out, "q", (N, Hq, c.D), q.dtype, dev)
-    ks = k.stride()
-    n = RelAppend(N, Hq, D, qs[0], qs[1], ks[0], ks[1], float(rope_base or 0.0), REL_GIVENS[pairing])
-    st = lib.relation_paged_append(ctypes.byref(c), ctypes.byref(n), _ptr(q), _ptr(k), _ptr(v), _ptr(slots),
-                                   _ptr(positions), _ptr(th), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream())
-    _check(st, "relation_paged_append")
+        Hq = q.shape[1]
+        qt, qh, _ = q.stride()
+        q_out = _given(out, "q", (N, Hq, c.D), q.dtype, dev)
+        if q_out is None:
+            q_out = q.new_empty((N, Hq, c.D))
+    n = RelAppend(N, Hq, D, qt, qh, ks[0], ks[1], float(rope_base or 0.0), givens)
+    st = lib.relation_paged_append(ctypes.byref(c), ctypes.byref(n), _ptr(q), k.data_ptr(), v.data_ptr(),
+                                   slots.data_ptr(), positions.data_ptr(), _ptr(th), _ptr(q_out), k_cache.data_ptr(),
+                                   v_cache.data_ptr(), _stream())
+    if st:
+        _check(st, "relation_paged_append")
     return q_out
 
 
@@ -759,35 +777,44 @@ def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_lengt
     multiple of H), table int32 [B, W], lengths int32 [B] (the new token's own entry last), max_length a bound of
     the lengths (default W * page_size). Returns dict(o [B, Hq, D], row_stat [B, Hq])."""
     lib = load_library()
-    dev = _on_gpu(q=q, k_cache=k_cache, v_cache=v_cache, table=table, lengths=lengths)
+    dev = _on_gpu(q, k_cache, v_cache, table, lengths)
     c = make_pages(k_cache, v_cache)
     if q.dim() != 3 or q.shape[2] != c.D or q.dtype != k_cache.dtype:
         raise ValueError("q must be [B, Hq, D] with the caches' width and dtype")
     B, Hq, D = q.shape
     if table.dim() != 2 or table.shape[0] != B or lengths.shape != (B,):
         raise ValueError("table must be [B, W] and lengths [B]")
-    q = q.contiguous()
-    table, lengths = _dense(table, dev, torch.int32), _dense(lengths, dev, torch.int32)
-    lam_t = _lam_tensor(lam, dev)
-    d = RelPagedQuery(B, Hq, table.shape[1], int(max_length or 0), float(tau_s), 0.0 if scale is None else float(scale))
-    o = _out(out, "o", (B, Hq, D), q.dtype, dev)
-    rs = _out(out, "row_stat", (B, Hq), torch.float32, dev)
-    ws = _workspace(int(lib.relation_paged_decode_workspace_bytes(ctypes.byref(c), ctypes.byref(d))), workspace, dev)
-    st = lib.relation_paged_decode(ctypes.byref(c), ctypes.byref(d), _ptr(q), _ptr(k_cache), _ptr(v_cache),
-                                   _ptr(table), _ptr(lengths), _ptr(lam_t), _ptr(o), _ptr(rs), _ptr(ws),
-                                   0 if ws is None else _nbytes(ws), _stream())
-    _check(st, "relation_paged_decode")
+    if not q.is_contiguous():
+        q = q.contiguous()
+    table, lengths = _ready(table, torch.int32), _ready(lengths, torch.int32)
+    lam_t = _lam_tensor(lam, q.device)
+    d = RelPagedQuery(B, Hq, table.shape[1], int(max_length or 0), tau_s, 0.0 if scale is None else scale)
+    o, rs = _given(out, "o", (B, Hq, D), q.dtype, dev), _given(out, "row_stat", (B, Hq), torch.float32, dev)
+    if o is None:
+        o = torch.empty_like(q)
+    if rs is None:
+        rs = q.new_empty((B, Hq), dtype=torch.float32)
+    need = lib.relation_paged_decode_workspace_bytes(ctypes.byref(c), ctypes.byref(d))
+    ws = _workspace(need, workspace, q.device) if need else None
+    st = lib.relation_paged_decode(ctypes.byref(c), ctypes.byref(d), q.data_ptr(), k_cache.data_ptr(),
+                                   v_cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), lam_t.data_ptr(),
+                                   o.data_ptr(), rs.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream())
+    if st:
+        _check(st, "relation_paged_decode")
     return {"o": o, "row_stat": rs}
 
 
-def _per_row(x, name, B, dtype, dev):
+def _per_row(x, name, B, dtype, logits):
+    """Pointer (None: off) and tensor of a sampling parameter."""
     if x is None:
-        return None
+        return None, None
     if not isinstance(x, torch.Tensor):
-        return torch.full((B,), x, dtype=dtype, device=dev)
-    if x.shape != (B,):
-        raise ValueError(f"{name} must be a number or [B]")
-    return _dense(x, dev, dtype)
+        x = logits.new_full((B,), x, dtype=dtype)
+    elif x.shape != (B,) or x.get_device() != logits.get_device():
+        raise ValueError(f"{name} must be a number, or [B] on the logits' GPU")
+    elif x.dtype != dtype or not x.is_contiguous():
+        x = x.detach().to(dtype).contiguous()
+    return x.data_ptr(), x
 
 
 def relation_sample(logits, noise, *, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, out=None):
@@ -795,25 +822,32 @@ def relation_sample(logits, noise, *, temperature=None, top_k=None, top_p=None, 
     temperature, top_k, top_p, min_p: numbers, [B] tensors, or None (off). Returns dict(tokens int64 [B],
     logprob fp32 [B]: log softmax(logits / temperature) of the token)."""
     lib = load_library()
-    dev = _on_gpu(logits=logits, noise=noise)
+    dev = _on_gpu(logits, noise)
     if logits.dim() != 2 or noise.shape != logits.shape or noise.dtype != torch.float32:
         raise ValueError("logits must be [B, V] and noise fp32 [B, V]")
     B, V = logits.shape
-    if V > 1 and logits.stride(1) != 1:
-        logits = logits.contiguous()
-    if V > 1 and noise.stride(1) != 1:
-        noise = noise.contiguous()
-    temperature = _per_row(temperature, "temperature", B, torch.float32, dev)
-    top_k = _per_row(top_k, "top_k", B, torch.int32, dev)
-    top_p, min_p = _per_row(top_p, "top_p", B, torch.float32, dev), _per_row(min_p, "min_p", B, torch.float32, dev)
-    s = RelSample(B, V, _dtype_code(logits.dtype), logits.stride(0), noise.stride(0))
-    tokens = _out(out, "tokens", (B,), torch.int64, dev)
-    logprob = _out(out, "logprob", (B,), torch.float32, dev)
-    ws = _workspace(int(lib.relation_sample_workspace_bytes(ctypes.byref(s))), workspace, dev)
-    st = lib.relation_sample(ctypes.byref(s), _ptr(logits), _ptr(noise), _ptr(temperature), _ptr(top_k), _ptr(top_p),
-                             _ptr(min_p), _ptr(tokens), _ptr(logprob), _ptr(ws), 0 if ws is None else _nbytes(ws),
-                             _stream())
-    _check(st, "relation_sample")
+    (sl, se), (sn, ne) = logits.stride(), noise.stride()
+    if V > 1 and se != 1:
+        logits, sl = logits.contiguous(), V
+    if V > 1 and ne != 1:
+        noise, sn = noise.contiguous(), V
+    f32 = torch.float32
+    pt, t1 = _per_row(temperature, "temperature", B, f32, logits)
+    pk, t2 = _per_row(top_k, "top_k", B, torch.int32, logits)
+    pp, t3 = _per_row(top_p, "top_p", B, f32, logits)
+    pm, t4 = _per_row(min_p, "min_p", B, f32, logits)
+    s = RelSample(B, V, _dtype_code(logits.dtype), sl, sn)
+    tokens, logprob = _given(out, "tokens", (B,), torch.int64, dev), _given(out, "logprob", (B,), f32, dev)
+    if tokens is None:
+        tokens = noise.new_empty(B, dtype=torch.int64)
+    if logprob is None:
+        logprob = noise.new_empty(B)
+    need = lib.relation_sample_workspace_bytes(ctypes.byref(s))
+    ws = _workspace(need, workspace, logits.device) if need else None
+    st = lib.relation_sample(ctypes.byref(s), logits.data_ptr(), noise.data_ptr(), pt, pk, pp, pm, tokens.data_ptr(),
+                             logprob.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream())
+    if st:
+        _check(st, "relation_sample")
     return {"tokens": tokens, "logprob": logprob}
 
 
