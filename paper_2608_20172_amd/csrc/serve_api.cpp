@@ -343,7 +343,7 @@ static rel_status check_sample(const rel_sample* s, bool* empty) {
 size_t relation_sample_workspace_bytes(const rel_sample* s) {
   bool empty = false;
   if (check_sample(s, &empty) != REL_OK || empty) return 0;
-  return rel::sample_workspace_bytes(s->B, s->V);
+  return rel::sample_workspace_bytes(s->B, s->V, s->dtype);
 }
 
 rel_status relation_sample(const rel_sample* s, const void* logits, const float* noise, const float* temperature,
@@ -352,7 +352,7 @@ rel_status relation_sample(const rel_sample* s, const void* logits, const float*
   bool empty = false;
   REL_TRY(check_sample(s, &empty));
   if (empty) return REL_OK;
-  const size_t need = rel::sample_workspace_bytes(s->B, s->V);
+  const size_t need = rel::sample_workspace_bytes(s->B, s->V, s->dtype);
   if (need && (!workspace || workspace_bytes < need))
     return api_fail(REL_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
   const size_t es = elem_size(s->dtype), B = (size_t)s->B;
