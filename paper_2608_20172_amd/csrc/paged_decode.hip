@@ -25,6 +25,7 @@ namespace rel {
 namespace {
 
 constexpr int kMergeT = 256;
+constexpr int kStatesT = 256;    // threads of the fp32 states kernel
 constexpr int kFewGroups = 512;  // workgroups (two per CU) below which they get more waves
 constexpr int kUnroll = 2;  // keys per lane group whose loads are in flight together
 
@@ -116,27 +117,31 @@ __device__ __forceinline__ void finish_row(const PagedDecodeArgs& a, int b, int 
   if (lane == 0 && a.row_stat) a.row_stat[(int64_t)b * a.Hq + hq] = s.ok ? lnZ + lam * ln_i : nan;
 }
 
-// Offsets of the slice's pages p0 .. p1 (of head h) into LDS, by all NT threads; whether the thread met a bad page.
+// Offsets (of head h) of the pages of slice [s0, s0 + slice) into LDS, by all NT
+// threads, and whether the thread met a bad page that holds keys before s1. The
+// table is read before s1, which hangs on the request's length, is looked at: the
+// two reads run side by side.
 template <int NT>
-__device__ __forceinline__ int page_offsets(const PagedDecodeArgs& a, int b, int h, int p0, int p1, int64_t* offs) {
+__device__ __forceinline__ int page_offsets(const PagedDecodeArgs& a, int b, int h, int s0, int len, int64_t* offs) {
+  const int p0 = s0 >> a.c.shift, p1 = min((s0 + a.slice - 1) >> a.c.shift, a.W - 1);
+  const int32_t* row = a.table + (int64_t)b * a.W;
   int bad = 0;
   for (int p = p0 + threadIdx.x; p <= p1; p += NT) {
-    const int id = a.table[(int64_t)b * a.W + p];
+    const int id = row[p];
     const bool ok = id >= 0 && id < a.c.num_pages;
     offs[p - p0] = (int64_t)(ok ? id : 0) * a.c.sp + (int64_t)h * a.c.sh;
-    bad |= !ok;
+    bad |= !ok && (p << a.c.shift) < len - 1;
   }
   return bad;
 }
 
 // One wave joins the NW waves' states of a row, (m, l, z) at st + wave * stride in
-// LDS, in the waves' order, and stores the slice's state or finishes the row.
+// LDS, in the waves' order, and stores the slice's state, or finishes the row with
+// its Self entry (one slice).
 template <typename TI, int NW>
 __device__ __forceinline__ void join_waves(const PagedDecodeArgs& a, int slice, int b, int hq, int len, int lane,
-                                           const float* st, int stride) {
+                                           const float* st, int stride, const SelfEntry& self) {
   const int D = a.c.D;
-  SelfEntry self;
-  if (a.nsplit == 1) self = read_self<TI>(a, b, hq, len, lane);
   float m = kNegInf, l = 0.0f, z[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int x = 0; x < NW; ++x) {
@@ -161,9 +166,13 @@ __device__ __forceinline__ void join_waves(const PagedDecodeArgs& a, int slice, 
 // head (workgroup = (request, key head, r, slice)). LPK lanes share a key: lane
 // c of the group holds VEC channels (16 bytes) of the queries and reads those
 // of the key and value rows; every lane group keeps its own running (m, l, z),
-// and the groups of the workgroup meet in LDS in a fixed order.
-template <int LPK, int GQ, int NT>
-__global__ __launch_bounds__(NT) void paged_states_f32_kernel(PagedDecodeArgs a) {
+// and the groups of the workgroup meet in LDS in a fixed order. Measured, 7
+// requests of 41 to 2047 tokens, 8 heads x 80 (37 MB): 12.5 us, 3.0 TB/s; the same
+// within 5% with 512 threads, slices of 64 keys, or four keys in flight; 19.4 with
+// 1024 threads.
+template <int LPK, int GQ>
+__global__ __launch_bounds__(kStatesT) void paged_states_f32_kernel(PagedDecodeArgs a) {
+  constexpr int NT = kStatesT;
   typedef float TI;
   constexpr int VEC = 4;
   constexpr int KPW = 64 / LPK;  // keys per wave and step
@@ -183,6 +192,9 @@ __global__ __launch_bounds__(NT) void paged_states_f32_kernel(PagedDecodeArgs a)
   const int len = length_of(a, b);
   const int s0 = slice * a.slice, s1 = min(s0 + a.slice, len - 1);  // Exchange keys only: j < i - 1 (zero-based)
   const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
+  int bad = page_offsets<NT>(a, b, h, s0, len, offs);
+  SelfEntry self{};
+  if (a.nsplit == 1 && w < ng) self = read_self<TI>(a, b, hq0 + w, len, lane);
   if (s1 <= s0 && a.nsplit > 1) return;  // a slice past the request's end: nobody reads its state
 
   float m[GQ], l[GQ], z[GQ][VEC];
@@ -194,7 +206,6 @@ __global__ __launch_bounds__(NT) void paged_states_f32_kernel(PagedDecodeArgs a)
     for (int e = 0; e < VEC; ++e) z[g][e] = 0.0f;
   }
   if (s1 > s0) {  // uniform in the workgroup
-    int bad = page_offsets<NT>(a, b, h, p0, (s1 - 1) >> a.c.shift, offs);
     float q[GQ][VEC];
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
@@ -275,7 +286,7 @@ __global__ __launch_bounds__(NT) void paged_states_f32_kernel(PagedDecodeArgs a)
   }
   __syncthreads();
   // wave g joins the waves' states of query head g
-  if (w < ng) join_waves<TI, NW>(a, slice, b, hq0 + w, len, lane, &red[0][w][0], GQ * (2 + 128));
+  if (w < ng) join_waves<TI, NW>(a, slice, b, hq0 + w, len, lane, &red[0][w][0], GQ * (2 + 128), self);
 }
 
 // The same in bf16 on the matrix cores, for up to 16 query heads of a key head
@@ -329,6 +340,9 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
   const int len = length_of(a, b);
   const int s0 = slice * a.slice, s1 = min(s0 + a.slice, len - 1);  // Exchange keys only: j < i - 1 (zero-based)
   const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
+  int bad = page_offsets<NW * 64>(a, b, h, s0, len, offs);
+  SelfEntry self{};
+  if (a.nsplit == 1 && w < ng) self = read_self<bf16>(a, b, hq0 + w, len, lane);
   if (s1 <= s0 && a.nsplit > 1) return;   // a slice past the request's end: nobody reads its state
 
   float m = kNegInf, l = 0.0f;
@@ -336,7 +350,6 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
 #pragma unroll
   for (int d = 0; d < DB; ++d) z[d] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
   if (s1 > s0) {  // uniform in the workgroup
-    int bad = page_offsets<NW * 64>(a, b, h, p0, (s1 - 1) >> a.c.shift, offs);
     const uintx4 none = {0, 0, 0, 0};
     bf16x8 q[KS];
     bool chan[KS];
@@ -458,8 +471,11 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
       for (int x = 0; x < 4; ++x) st[r * SW + 2 + 16 * d + 4 * g + x] = z[d][x];
   }
   __syncthreads();
-  for (int y = w; y < ng; y += NW)
-    join_waves<bf16, NW>(a, slice, b, hq0 + y, len, lane, reinterpret_cast<const float*>(vlds[0]) + y * SW, WAVEB / 4);
+  for (int y = w; y < ng; y += NW) {
+    if (a.nsplit == 1 && y >= NW) self = read_self<bf16>(a, b, hq0 + y, len, lane);
+    join_waves<bf16, NW>(a, slice, b, hq0 + y, len, lane, reinterpret_cast<const float*>(vlds[0]) + y * SW, WAVEB / 4,
+                         self);
+  }
 }
 
 // One workgroup per (b, query head): joins the row's states. Only the slices
@@ -521,9 +537,8 @@ size_t offsets_bytes(const PagedDecodeArgs& a) { return (size_t)((a.slice >> a.c
 
 template <int LPK, int GQ>
 void launch_f32(const PagedDecodeArgs& a, hipStream_t stream) {
-  constexpr int NT = 256;
   const int64_t grid = (int64_t)a.nsplit * a.B * a.c.H * ((a.G + GQ - 1) / GQ);
-  hipLaunchKernelGGL((paged_states_f32_kernel<LPK, GQ, NT>), dim3((unsigned)grid), dim3(NT), offsets_bytes(a), stream, a);
+  hipLaunchKernelGGL((paged_states_f32_kernel<LPK, GQ>), dim3((unsigned)grid), dim3(kStatesT), offsets_bytes(a), stream, a);
 }
 template <int LPK>
 void launch_f32_g(const PagedDecodeArgs& a, hipStream_t stream) {
