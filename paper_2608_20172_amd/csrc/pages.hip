@@ -160,45 +160,48 @@ __global__ __launch_bounds__(kMapT) void page_map_kernel(PageMapArgs a) {
 // context keeps its fraction), then the rows of all heads are moved by threads
 // that hold a chunk of the first half and the one it turns with. Every channel
 // is read and written once: bound by memory.
+// Chunks are of 16 bytes whatever the width and the alignment: the last chunk of
+// a half is moved back to end with it, and repeats some channels of the one before
+// (the same values into the same places). 16384 tokens of 12 heads in bf16: width
+// 64 33 us (151 MB, 4.6 TB/s); width 60 in a cache of 64 51 us (147 MB), 64 with
+// 4-byte chunks, which divide a half of 30.
 // ---------------------------------------------------------------------------
 constexpr int kAppT = 256;
-constexpr int kAppMaxTokens = 16;
+constexpr int kAppMaxTokens = 8;
 
+// VEC elements (16 bytes, or one) on any element boundary, as floats.
 template <typename TI, int VEC>
 __device__ __forceinline__ void load_vec(const TI* p, float (&x)[VEC]) {
   if constexpr (VEC == 1) {
     x[0] = (float)*p;
-  } else if constexpr (sizeof(TI) == 2) {  // pairs from whole words
-    typedef unsigned int U __attribute__((ext_vector_type(VEC / 2 > 1 ? VEC / 2 : 2)));
-    if constexpr (VEC == 2) {
-      const unsigned int u = *reinterpret_cast<const unsigned int*>(p);
-      x[0] = bf16_lo(u);
-      x[1] = bf16_hi(u);
-    } else {
-      const U u = *reinterpret_cast<const U*>(p);
+  } else if constexpr (sizeof(TI) == 2) {
+    typedef unsigned int U __attribute__((ext_vector_type(4), aligned(2)));
+    const U u = *reinterpret_cast<const U*>(p);
 #pragma unroll
-      for (int e = 0; e < VEC / 2; ++e) {
-        x[2 * e] = bf16_lo(u[e]);
-        x[2 * e + 1] = bf16_hi(u[e]);
-      }
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = bf16_lo(u[e]);
+      x[2 * e + 1] = bf16_hi(u[e]);
     }
   } else {
-    typedef TI V __attribute__((ext_vector_type(VEC)));
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     const V u = *reinterpret_cast<const V*>(p);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = u[e];
+    for (int e = 0; e < 4; ++e) x[e] = u[e];
   }
 }
 template <typename TI, int VEC>
 __device__ __forceinline__ void store_vec(TI* p, const float (&x)[VEC]) {
-  typedef TI V __attribute__((ext_vector_type(VEC)));
   if constexpr (VEC == 1) {
     *p = (TI)x[0];
-  } else {
-    V u;
+  } else if constexpr (sizeof(TI) == 2) {
+    typedef unsigned int U __attribute__((ext_vector_type(4), aligned(2)));
+    bf16x8 o;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) u[e] = (TI)x[e];
-    *reinterpret_cast<V*>(p) = u;
+    for (int e = 0; e < 8; ++e) o[e] = (bf16)x[e];
+    *reinterpret_cast<U*>(p) = __builtin_bit_cast(uintx4, o);
+  } else {
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+    *reinterpret_cast<V*>(p) = V{x[0], x[1], x[2], x[3]};
   }
 }
 
@@ -226,8 +229,8 @@ __global__ __launch_bounds__(kAppT) void append_kernel(AppendArgs a, int tpw) {
   }
   __syncthreads();
   const int nq = a.q ? a.Hq : 0, heads = nq + a.c.H;
-  // q and k: tasks (token, head, chunk of the first part); without RoPE the parts are chunks VEC apart
-  const int ch = a.rope ? half / VEC : a.D / VEC;  // chunks per row
+  // q and k: tasks (token, head, chunk), a chunk of each half with RoPE
+  const int run = a.rope ? half : a.D, ch = (run + VEC - 1) / VEC;
   for (int i = tid; i < nt * heads * ch; i += kAppT) {
     const int c = i % ch, nh = i / ch, h = nh % heads, n = nh / heads;
     const bool isq = h < nq;
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(kAppT) void append_kernel(AppendArgs a, int tpw) {
     const TI* src = isq ? (const TI*)a.q + (n0 + n) * a.q_token + h * a.q_head
                         : (const TI*)a.k + (n0 + n) * a.kv_token + hk * a.kv_head;
     TI* dst = isq ? (TI*)a.q_out + ((int64_t)(n0 + n) * a.Hq + h) * Dc : (TI*)a.k_cache + r0 + (int64_t)hk * a.c.sh;
-    const int e0 = c * VEC;
+    const int e0 = min(c * VEC, run - VEC);
     float x[VEC], y[VEC];
     load_vec<TI, VEC>(src + e0, x);
     if (a.rope) {
@@ -264,13 +267,14 @@ __global__ __launch_bounds__(kAppT) void append_kernel(AppendArgs a, int tpw) {
     }
   }
   // v: a head pair's chunk with Givens mixing, else one head's
-  const int vch = a.D / VEC, vh = a.givens ? a.c.H / 2 : a.c.H;
+  const int vch = (a.D + VEC - 1) / VEC, vh = a.givens ? a.c.H / 2 : a.c.H;
   for (int i = tid; i < nt * vh * vch; i += kAppT) {
     const int c = i % vch, nh = i / vch, h = nh % vh, n = nh / vh;
     const int64_t r0 = row0[n];
     if (r0 < 0) continue;
-    const TI* src = (const TI*)a.v + (n0 + n) * a.kv_token + c * VEC;
-    TI* dst = (TI*)a.v_cache + r0 + c * VEC;
+    const int e0 = min(c * VEC, a.D - VEC);
+    const TI* src = (const TI*)a.v + (n0 + n) * a.kv_token + e0;
+    TI* dst = (TI*)a.v_cache + r0 + e0;
     float x[VEC], y[VEC];
     if (a.givens) {
       const int p = 2 * h + (a.givens == 2 ? 1 : 0), p2 = p + 1 == a.c.H ? 0 : p + 1;
@@ -291,22 +295,26 @@ __global__ __launch_bounds__(kAppT) void append_kernel(AppendArgs a, int tpw) {
       store_vec<TI, VEC>(dst + (int64_t)h * a.c.sh, x);
     }
   }
-  // zeros in channels D .. Dc - 1
-  const int pad = Dc - a.D, ph = nq + 2 * a.c.H;
+  // zeros in channels D .. Dc - 1, as words where the element is half a word and D even
+  const int words = sizeof(TI) == 2 && a.D % 2 == 0;
+  const int pad = words ? (Dc - a.D) / 2 : Dc - a.D, ph = nq + 2 * a.c.H;
   for (int i = tid; i < nt * ph * pad; i += kAppT) {
-    const int e = a.D + i % pad, nh = i / pad, h = nh % ph, n = nh / ph;
+    const int e = a.D + (i % pad << words), nh = i / pad, h = nh % ph, n = nh / ph;
     const int64_t r0 = row0[n];
-    if (h < nq)
-      ((TI*)a.q_out)[((int64_t)(n0 + n) * a.Hq + h) * Dc + e] = (TI)0.0f;
-    else if (r0 >= 0)
-      (h < nq + a.c.H ? (TI*)a.k_cache + (int64_t)(h - nq) * a.c.sh : (TI*)a.v_cache + (int64_t)(h - nq - a.c.H) * a.c.sh)
-          [r0 + e] = (TI)0.0f;
+    if (h >= nq && r0 < 0) continue;
+    TI* dst = h < nq            ? (TI*)a.q_out + ((int64_t)(n0 + n) * a.Hq + h) * Dc
+              : h < nq + a.c.H  ? (TI*)a.k_cache + r0 + (int64_t)(h - nq) * a.c.sh
+                                : (TI*)a.v_cache + r0 + (int64_t)(h - nq - a.c.H) * a.c.sh;
+    if (words)
+      *reinterpret_cast<unsigned int*>(dst + e) = 0;
+    else
+      dst[e] = (TI)0.0f;
   }
 }
 
 template <typename TI, int VEC>
 hipError_t append_t(const AppendArgs& a, hipStream_t stream) {
-  const int tpw = a.N >= 4096 ? 8 : 1;
+  const int tpw = a.N >= 4096 ? kAppMaxTokens : 1;
   hipLaunchKernelGGL((append_kernel<TI, VEC>), dim3((unsigned)((a.N + tpw - 1) / tpw)), dim3(kAppT),
                      (size_t)tpw * (a.D / 2) * sizeof(float2), stream, a, tpw);
   return hipGetLastError();
@@ -322,13 +330,10 @@ hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_append(const AppendArgs& a, int dtype, int vec, hipStream_t stream) {
-  if (dtype == 1) {
-    if (vec == 8) return append_t<bf16, 8>(a, stream);
-    return vec == 2 ? append_t<bf16, 2>(a, stream) : append_t<bf16, 1>(a, stream);
-  }
-  if (vec == 4) return append_t<float, 4>(a, stream);
-  return vec == 2 ? append_t<float, 2>(a, stream) : append_t<float, 1>(a, stream);
+hipError_t launch_append(const AppendArgs& a, int dtype, hipStream_t stream) {
+  const int run = a.rope ? a.D / 2 : a.D, vec = dtype == 1 ? 8 : 4;
+  if (run >= vec) return dtype == 1 ? append_t<bf16, 8>(a, stream) : append_t<float, 4>(a, stream);
+  return dtype == 1 ? append_t<bf16, 1>(a, stream) : append_t<float, 1>(a, stream);  // narrower than a chunk
 }
 
 }  // namespace rel

@@ -52,8 +52,7 @@ struct AppendArgs {
   int rope;            // 1: rotate q and k
   double turns[64];    // turns of channel pair j per position: base^(-2j/D) / (2 pi)
 };
-// vec: contiguous channels that a thread moves (8, 2 or 1 for bf16; 4, 2 or 1 for fp32).
-hipError_t launch_append(const AppendArgs& a, int dtype, int vec, hipStream_t stream);
+hipError_t launch_append(const AppendArgs& a, int dtype, hipStream_t stream);
 
 struct PagedDecodeArgs {
   const void* q;           // [B, Hq, D] dense

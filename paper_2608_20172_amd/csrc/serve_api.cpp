@@ -252,19 +252,7 @@ rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const 
   if (a.rope)
     for (int j = 0; j < a.D / 2; ++j)
       a.turns[j] = std::exp(-2.0 * j / a.D * std::log(n->rope_base)) / 6.283185307179586476925286766559;
-  // the widest chunk that the rows allow: 16 bytes, two channels, or one
-  const int wide = (int)(16 / es);
-  int vec = 1;
-  for (int x : {wide, 2}) {
-    bool ok = n->D % x == 0 && (!a.rope || (n->D / 2) % x == 0) && n->kv_token % x == 0 && n->kv_head % x == 0;
-    ok = ok && (uintptr_t)k % (x * es) == 0 && (uintptr_t)v % (x * es) == 0;
-    if (has_q) ok = ok && n->q_token % x == 0 && n->q_head % x == 0 && (uintptr_t)q % (x * es) == 0;
-    if (ok) {
-      vec = x;
-      break;
-    }
-  }
-  return hip_status(rel::launch_append(a, c->dtype, vec, (hipStream_t)stream), "paged append launch");
+  return hip_status(rel::launch_append(a, c->dtype, (hipStream_t)stream), "paged append launch");
 }
 
 size_t relation_paged_decode_workspace_bytes(const rel_pages* c, const rel_paged_query* d) {
