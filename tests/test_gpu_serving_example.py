@@ -1,0 +1,45 @@
+"""The serving example end to end: prompts and decode steps through the paged
+cache give the hidden rows that the whole sequences give, and the same tokens
+whatever the page size."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from examples import serve_paged as E
+
+pytestmark = pytest.mark.gpu
+
+# Both paths round the rotated operands, the outputs and the residual to bf16 in each of two layers, in other
+# places: relative 2^-8 a rounding, eight of them, at their square root and doubled.
+BAR = 2.0 ** -8 * 8 ** 0.5 * 2
+
+
+@pytest.fixture(scope="module")
+def model():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return E.Decoder(vocab=3001, layers=2, heads=4, width=64)
+
+
+def _prompts(model, lens):
+    g = torch.Generator(device="cuda").manual_seed(7)
+    return [torch.randint(0, model.emb.shape[0], (n,), device="cuda", generator=g) for n in lens]
+
+
+@pytest.mark.parametrize("page", [8, 32])
+def test_decode_steps_are_the_whole_sequence(model, page):
+    prompts = _prompts(model, (1, 15, 33, 290))
+    tokens, logprob, x = E.generate(model, prompts, 20, page_size=page, temperature=0.8, top_k=50, top_p=0.9)
+    torch.cuda.synchronize()
+    err = E.check(model, prompts, tokens, x)
+    print(f"page {page}: relative 2-norm {err:.2e} (bar {BAR:.2e})", flush=True)
+    assert err <= BAR
+    assert tokens.shape == (4, 20) and int(tokens.min()) >= 0 and int(tokens.max()) < 3001
+    assert bool((logprob <= 0).all())
+
+
+def test_page_size_changes_nothing(model):
+    prompts = _prompts(model, (5, 64))
+    a, b = (E.generate(model, prompts, 12, page_size=p, temperature=0.0)[0] for p in (16, 64))
+    assert torch.equal(a, b)
