@@ -321,6 +321,12 @@ __device__ __forceinline__ bf16x8 pack8(const float (&x)[8]) {
   return o;
 }
 
+// Orders a wave's LDS accesses for the compiler; in the hardware they keep their order as they are.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <int DB, int NW>
 __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeArgs a) {
   constexpr int KS = (DB + 1) / 2;        // products of 32 channels
@@ -390,10 +396,12 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
     };
     if (s0 + 32 * w < s1) load(s0 + 32 * w);
     for (int base = s0 + 32 * w; base < s1; base += 32 * NW) {
-      // K through LDS into operands, then V into the same place: a wave's LDS accesses keep their order
+      // K through LDS into operands, then V into the same place
+      wave_order();
 #pragma unroll
       for (int i = 0; i < DB; ++i)
         if (i < nld) *reinterpret_cast<uintx4*>(vlds[w] + krow[i] * ROWB + kcol[i] * 16) = kx[i];
+      wave_order();
       floatx4_t u[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -405,9 +413,11 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
           u[t] = mfma16(__builtin_bit_cast(bf16x8, x), q[s], u[t]);
         }
       }
+      wave_order();
 #pragma unroll
       for (int i = 0; i < DB; ++i)
         if (i < nld) *reinterpret_cast<uintx4*>(vlds[w] + krow[i] * ROWB + kcol[i] * 16) = vx[i];
+      wave_order();
       // the registers are free: the next keys' loads run beside the rest of this step
       if (base + 32 * NW < s1) load(base + 32 * NW);
       float e[8];
@@ -458,6 +468,7 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
     l += __shfl_xor(l, 32, 64);
   }
   // the wave's state of query r into its LDS: m, l, z
+  wave_order();
   constexpr int SW = 2 + 16 * DB;
   float* st = reinterpret_cast<float*>(vlds[w]);
   if (r < ng) {
