@@ -65,6 +65,7 @@ struct PagedDecodeArgs {
   int B, Hq, G, W;         // Hq = G * c.H
   int max_len;             // lengths above it are refused (NaN)
   int nsplit, slice;       // slices of `slice` keys
+  int placed;              // 1: workgroups that share cache lines on one die (set by the launch)
   float scale, inv_tau;
   float* states;           // [nsplit][B Hq][D + 2] (nsplit > 1)
   void* out;               // [B, Hq, D] dense

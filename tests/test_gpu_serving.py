@@ -213,6 +213,18 @@ def test_paged_decode(lens, H, G, D, page, dtype, layout):
             assert torch.equal(r["o"][b], vc[table[b, 0], :, 0].repeat_interleave(G, 0))
 
 
+@pytest.mark.parametrize("B,H,G,D,dtype", [(64, 3, 1, 48, "bf16"), (67, 2, 17, 80, "bf16"), (71, 3, 1, 40, "f32"),
+                                           (65, 2, 6, 20, "f32")])
+def test_paged_decode_heads_that_share_lines(B, H, G, D, dtype):
+    """Heads side by side in rows that are no multiple of 128 bytes, with over 64 slices and requests: groups of
+    workgroups are placed, 64 of them to 71 (full turns of eight and broken ones), one slice a row and several."""
+    for top in (200, 700):
+        lens = [1 + (37 * b) % top for b in range(B)]
+        log(f"[paged_decode] placed B={B} H={H} G={G} D={D} {dtype} up to {top}")
+        r, Y, M, _ = _decode_case(lens, H, G, D, 16, dtype, "nhd")
+        _decode_close(r, Y, M, dtype)
+
+
 def test_paged_decode_long():
     """One request of 40000 tokens, 4 heads of width 128: many slices, 157 of them of 256 keys."""
     r, Y, M, _ = _decode_case([40000, 3], 4, 1, 128, 64, "bf16", "nhd")
