@@ -225,6 +225,17 @@ def test_paged_decode_heads_that_share_lines(B, H, G, D, dtype):
         _decode_close(r, Y, M, dtype)
 
 
+@pytest.mark.parametrize("B,H,G,D,top,page,dtype", [(300, 8, 1, 32, 1500, 16, "bf16"), (40, 8, 2, 64, 5000, 1, "bf16"),
+                                                    (150, 8, 1, 32, 1400, 32, "f32"), (24, 16, 1, 128, 3300, 256, "bf16")])
+def test_paged_decode_many_rows(B, H, G, D, top, page, dtype):
+    """So many rows that a slice is long: one of 4096 keys a row, several of 512 to 2048, offsets of 2048 pages of one
+    token."""
+    lens = [1 + (top * (b + 1) // B * 7919) % top for b in range(B)]
+    log(f"[paged_decode] many rows B={B} H={H} G={G} D={D} up to {max(lens)} page={page} {dtype}")
+    r, Y, M, _ = _decode_case(lens, H, G, D, page, dtype, "hnd")
+    _decode_close(r, Y, M, dtype)
+
+
 def test_paged_decode_long():
     """One request of 40000 tokens, 4 heads of width 128: many slices, 157 of them of 256 keys."""
     r, Y, M, _ = _decode_case([40000, 3], 4, 1, 128, 64, "bf16", "nhd")
@@ -394,6 +405,34 @@ def test_sample_parameters():
         mp = rng.choice([0.0, 0.0, -1.0, 0.001, 0.1, 1.0, 2.0], B)
         log(f"[sample] parameters {dtype}")
         _check_sample(x, r, T, k.tolist(), p, mp)
+
+
+@pytest.mark.parametrize("B,V,dtype,ranked", [(40, 60001, "f32", False), (33, 70007, "bf16", True), (2, 600011, "bf16", False),
+                                              (1, 2097152, "f32", False)])
+def test_sample_whole_chunks(B, V, dtype, ranked):
+    """Rows in chunks of 8192: many of them, or very long ones; every row its own filters, flat nuclei among them."""
+    rng = np.random.default_rng(26 + V)
+    x, r = _logits(B, V, dtype, rng, slope=1.1, ranked=ranked), _noise(B, V, rng)
+    log(f"[sample] whole chunks B={B} V={V} {dtype} ranked={ranked}")
+    T = rng.choice([0.0, 0.6, 1.0, 1.3], B)
+    k = rng.choice([0, 0, 1, 40, 1000, 20000], B)
+    p = rng.choice([1.0, 0.3, 0.9, 0.97], B)
+    mp = rng.choice([0.0, 0.0, 0.001, 0.1], B)
+    _check_sample(x, r, T, k.tolist(), p, mp)
+    _check_sample(x, r, 1.3, 0, 0.9, 0.0)
+    _check_sample(x, r)
+
+
+def test_sample_is_the_same_every_time():
+    """The same bits in every run, whatever the order in which workgroups and waves arrive."""
+    rng = np.random.default_rng(27)
+    for B, V, dtype in ((3, 5000, "bf16"), (5, 50257, "f32"), (64, 40000, "bf16")):
+        x, r = _logits(B, V, dtype, rng), _noise(B, V, rng)
+        par = dict(temperature=1.2, top_k=None, top_p=0.93, min_p=None)
+        a = R.relation_sample(x, r, **par)
+        for _ in range(4):
+            b = R.relation_sample(x, r, **par)
+            assert torch.equal(a["tokens"], b["tokens"]) and torch.equal(a["logprob"], b["logprob"])
 
 
 @pytest.mark.parametrize("V", [600, 20000, 131072])
