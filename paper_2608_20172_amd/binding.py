@@ -657,6 +657,13 @@ def _on_gpu(first, *rest) -> int:
     return dev
 
 
+def _stream_on(dev: int) -> int:
+    """The current stream, on the GPU that the tensors are on."""
+    if torch.cuda.current_device() != dev:
+        raise ValueError(f"the tensors are on GPU {dev}, the current one is {torch.cuda.current_device()}")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
 def _given(out, name, shape, dtype, dev):
     """out[name] where the caller gives it (checked), or None."""
     t = None if out is None else out.get(name)
@@ -714,7 +721,7 @@ def relation_page_map(cached, added, table, free_pages, page_size: int, max_toke
     m = RelPageMap(B, W, int(page_size), N, free_pages.shape[0])
     st = lib.relation_page_map(ctypes.byref(m), cached.data_ptr(), added.data_ptr(), free_pages.data_ptr(),
                                table.data_ptr(), lengths.data_ptr(), row_start.data_ptr(), slots.data_ptr(),
-                               positions.data_ptr(), counts.data_ptr(), _stream())
+                               positions.data_ptr(), counts.data_ptr(), _stream_on(dev))
     if st:
         _check(st, "relation_page_map")
     return {"table": table, "lengths": lengths, "row_start": row_start, "slots": slots, "positions": positions,
@@ -765,7 +772,7 @@ def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, t
     n = RelAppend(N, Hq, D, qt, qh, ks[0], ks[1], float(rope_base or 0.0), givens)
     st = lib.relation_paged_append(ctypes.byref(c), ctypes.byref(n), _ptr(q), k.data_ptr(), v.data_ptr(),
                                    slots.data_ptr(), positions.data_ptr(), _ptr(th), _ptr(q_out), k_cache.data_ptr(),
-                                   v_cache.data_ptr(), _stream())
+                                   v_cache.data_ptr(), _stream_on(dev))
     if st:
         _check(st, "relation_paged_append")
     return q_out
@@ -798,7 +805,7 @@ def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_lengt
     ws = _workspace(need, workspace, q.device) if need else None
     st = lib.relation_paged_decode(ctypes.byref(c), ctypes.byref(d), q.data_ptr(), k_cache.data_ptr(),
                                    v_cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), lam_t.data_ptr(),
-                                   o.data_ptr(), rs.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream())
+                                   o.data_ptr(), rs.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream_on(dev))
     if st:
         _check(st, "relation_paged_decode")
     return {"o": o, "row_stat": rs}
@@ -845,7 +852,7 @@ def relation_sample(logits, noise, *, temperature=None, top_k=None, top_p=None, 
     need = lib.relation_sample_workspace_bytes(ctypes.byref(s))
     ws = _workspace(need, workspace, logits.device) if need else None
     st = lib.relation_sample(ctypes.byref(s), logits.data_ptr(), noise.data_ptr(), pt, pk, pp, pm, tokens.data_ptr(),
-                             logprob.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream())
+                             logprob.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream_on(dev))
     if st:
         _check(st, "relation_sample")
     return {"tokens": tokens, "logprob": logprob}
