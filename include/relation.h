@@ -515,7 +515,8 @@ rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const 
  * max_length bounds the lengths of this call and with them the launch and the
  * workspace; <= 0 takes table_width * page_size. A request whose length is
  * outside 1 .. that bound, or one of whose pages is not in the pool, gets NaN
- * rows in out and row_stat. Entries past a request's length are not read. */
+ * rows in out and row_stat. Entries past a request's length are not read. An
+ * infinite value in the history may come out as NaN in its channel. */
 typedef struct rel_paged_query {
   int64_t B, Hq, table_width, max_length;
   float tau_s, scale; /* as in rel_problem; scale <= 0: 1/sqrt(c->D) */

@@ -26,9 +26,12 @@ namespace {
 
 constexpr int kMergeT = 256;
 constexpr int kStatesT = 256;    // threads of the fp32 states kernel
-constexpr int kDies = 8, kPlaced = 64;
-constexpr int kFewGroups = 512;  // workgroups (two per CU) below which they get more waves
-constexpr int kUnroll = 2;  // keys per lane group whose loads are in flight together
+constexpr int kDies = 8;         // L2 caches of the chip
+constexpr int kPlaced = 64;      // groups from which on they are placed by die
+// Workgroups (two per CU) below which the bf16 kernel gives them 8 waves instead of 4: 8 of 400 keys x 64 8.5 and 9.8
+// us, 128 of 512 9.4 and 10.5. With more workgroups the 8 waves' LDS costs more: 1024 of width 128 189 and 181.
+constexpr int kFewGroups = 512;
+constexpr int kUnroll = 2;       // keys per lane group of the fp32 kernel whose loads are in flight together
 
 struct Row {
   static __device__ __forceinline__ void load(const float* p, float (&x)[4]) {
@@ -147,9 +150,9 @@ __device__ __forceinline__ void finish_row(const PagedDecodeArgs& a, int b, int 
 }
 
 // Offsets (of head h) of the pages of slice [s0, s0 + slice) into LDS, by all NT
-// threads, and whether the thread met a bad page that holds keys before s1. The
-// table is read before s1, which hangs on the request's length, is looked at: the
-// two reads run side by side.
+// threads, and whether the thread met a bad page that holds keys of the request's
+// history. The table is read before the length is looked at: the two reads run side
+// by side.
 template <int NT>
 __device__ __forceinline__ int page_offsets(const PagedDecodeArgs& a, int b, int h, int s0, int len, int64_t* offs) {
   const int p0 = s0 >> a.c.shift, p1 = min((s0 + a.slice - 1) >> a.c.shift, a.W - 1);
@@ -613,14 +616,20 @@ hipError_t launch_merge(const PagedDecodeArgs& a, hipStream_t stream) {
 }  // namespace
 
 // Slices of the history: about kTargetGroups workgroups, of at least kMinSlice
-// keys; a history of up to kOneSlice is not split, and its rows need no second
-// launch.
-void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int* slice, int* nsplit) {
-  constexpr int64_t kTargetGroups = 1536, kMinSlice = 128, kMaxSlice = 4096, kOneSlice = 256;
+// keys (64 requests x 12 heads x 64 of up to 4096: slices of 512 94 us, 1024 96, 2048
+// 99, 4096 115; 2 x 16 x 128 of up to 65536: 193, 189, 181, 214; 1 x 8 x 128 of 4096:
+// 128 7.7, 256 10.0). A short history is not split and needs no second launch: one
+// slice against states and merge, 8 heads, bf16: 1000 keys x 64 10.9 and 6.1 + 4.6
+// us (16 requests 12.4 and 12.8 + 4.0); 500 x 128 11.4 and 7.4 + 4.3; 1000 x 128 15.4
+// and 7.4 + 4.9; fp32, 250 x 64 8.7 and 6.1 + 4.3; 500 x 64, 16 requests, 16.2 and
+// 9.4 + 4.0.
+void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype, int* slice, int* nsplit) {
+  constexpr int64_t kTargetGroups = 1536, kMinSlice = 128, kMaxSlice = 4096;
   const int64_t hist = max_len > 1 ? max_len - 1 : 1, rows = B * H * ((G + 15) / 16);
+  const int64_t one = dtype == 1 ? (D <= 64 ? 1024 : 512) : 256;
   int64_t s = kMinSlice;
   while (s < kMaxSlice && s * kTargetGroups < hist * rows) s *= 2;
-  if (hist <= kOneSlice) s = kOneSlice;
+  if (hist <= one) s = one;
   *slice = (int)s;
   *nsplit = (int)((hist + s - 1) / s);
 }

@@ -10,7 +10,7 @@
 // wins with probability w_i / sum of the kept w). So the race is run over all
 // tokens, its winner is looked up in the order by one sum, and if it is not kept,
 // nothing after it is either, and the race is run again over the tokens before
-// it. The sum and the next race are one pass.
+// it. Over a list the sum and the next race are one pass.
 //
 // Short rows (8192 fp32 logits, 16384 bf16) are held by one workgroup each, in one
 // launch. Longer ones are read once, by many workgroups a row (scan): each holds its

@@ -72,7 +72,7 @@ struct PagedDecodeArgs {
   float* row_stat;         // [B, Hq] or null
 };
 // Slices of a step: slice length and their number, by the host's bounds alone.
-void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int* slice, int* nsplit);
+void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype, int* slice, int* nsplit);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, hipStream_t stream);
 
 struct SampleArgs {

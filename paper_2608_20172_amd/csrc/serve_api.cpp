@@ -259,7 +259,7 @@ size_t relation_paged_decode_workspace_bytes(const rel_pages* c, const rel_paged
   bool empty = false;
   if (check_query(c, d, &empty) != REL_OK || empty) return 0;
   int slice = 0, nsplit = 0;
-  rel::paged_decode_split(d->B, c->H, d->Hq / c->H, longest(c, d), &slice, &nsplit);
+  rel::paged_decode_split(d->B, c->H, d->Hq / c->H, longest(c, d), (int)c->D, c->dtype, &slice, &nsplit);
   if (nsplit == 1) return 0;
   return (size_t)nsplit * (size_t)(d->B * d->Hq) * (size_t)(c->D + 2) * 4;
 }
@@ -274,7 +274,7 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
   rel::PagedDecodeArgs a{};
   a.max_len = (int)longest(c, d);
   a.G = (int)(d->Hq / c->H);
-  rel::paged_decode_split(d->B, c->H, a.G, a.max_len, &a.slice, &a.nsplit);
+  rel::paged_decode_split(d->B, c->H, a.G, a.max_len, (int)c->D, c->dtype, &a.slice, &a.nsplit);
   if ((int64_t)a.nsplit * d->B * d->Hq > (1 << 22))
     return api_fail(REL_ERR_UNSUPPORTED, "%lld rows of up to %d tokens are over 2^22 slices: pass max_length, or fewer requests",
                     (long long)(d->B * d->Hq), a.max_len);

@@ -129,10 +129,10 @@ def test_decode_arguments(lib):
     for n in ("q", "kc", "vc", "table", "lengths", "lam", "out"):
         assert decode(lib, **{n: None}) == BAD
         assert decode(lib, **{n: A[12] + 2}) == BAD
-    assert decode(lib, stat=None) == HIP and decode(lib, q=A[12] + 8) == BAD and decode(lib, ws=A[12] + 8) == BAD
+    assert decode(lib, stat=None) == HIP and decode(lib, q=A[12] + 8) == BAD and decode(lib, W=400, ws=A[12] + 8) == BAD
     for n in ("q", "kc", "vc", "table", "lengths", "lam"):
         assert decode(lib, out=A["q kc vc table lengths lam".split().index(n)]) == BAD
-    assert decode(lib, stat=A[6]) == BAD and decode(lib, ws=A[1]) == BAD
+    assert decode(lib, stat=A[6]) == BAD and decode(lib, W=400, ws=A[1]) == BAD
 
 
 def test_decode_workspace(lib):
