@@ -467,7 +467,7 @@ static rel_status fwd_impl(const rel_problem* p, const void* q, const void* k, c
                             {self_mass, rb, false, true, "self_mass"},
                             {exch_mass, rb, false, true, "exch_mass"},
                             {exch_lse, rb, false, true, "exch_lse"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::FwdArgs a{};
   a.q = q; a.k = k; a.v = v; a.lambda = lambda; a.o = o;
   a.row_stat = row_stat; a.self_mass = self_mass; a.exch_mass = exch_mass; a.exch_lse = exch_lse;
@@ -504,7 +504,7 @@ rel_status relation_exchange_allocation(const rel_problem* p, const void* q, con
                             {k, tb, true, false, "k"},
                             {exch_lse, rb, false, false, "exch_lse"},
                             {pi, mb, false, true, "pi"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::RowArgs a{};
   a.q = q; a.k = k; a.exch_lse = exch_lse; a.pi = pi;
   a.sb = p->stride_b; a.sh = p->stride_h; a.st = p->stride_t;
@@ -555,7 +555,7 @@ static rel_status bwd_impl(const rel_problem* p, const void* q, const void* k, c
   if (empty) {
     if (dlambda) {
       // nothing to differentiate: dlambda is still an output and must be zero
-      if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected");
+      if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected");
       hipError_t e = rel::launch_fill_zero(dlambda, 1, (hipStream_t)stream);
       if (e != hipSuccess) return hip_fail(e, "relation_bwd dlambda clear");
     }
@@ -594,7 +594,7 @@ static rel_status bwd_impl(const rel_problem* p, const void* q, const void* k, c
                             {dlambda, 4, false, true, "dlambda"},
                             {dself, rb, false, true, "dself"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   const size_t N = (size_t)(p->B * p->H);
   rel::BwdArgs a{};
   a.q = q; a.k = k; a.v = v; a.o = o; a.dout = dout; a.lambda = lambda; a.row_stat = row_stat;
@@ -742,7 +742,7 @@ rel_status relation_fwd_materialized(const rel_problem* p, const void* q, const 
                             {self_mass, rb, false, true, "self_mass"},
                             {exch_mass, rb, false, true, "exch_mass"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
 
   const int T = (int)p->T, D = (int)p->D;
   const float scale = eff_scale(p);
@@ -812,7 +812,7 @@ rel_status relation_bwd_materialized(const rel_problem* p, const void* q, const 
   REL_TRY(check_problem(p, &empty));
   if (empty) {
     if (dlambda) {
-      if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected");
+      if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected");
       hipError_t e = rel::launch_fill_zero(dlambda, 1, (hipStream_t)stream);
       if (e != hipSuccess) return hip_fail(e, "relation_bwd_materialized dlambda clear");
     }
@@ -846,7 +846,7 @@ rel_status relation_bwd_materialized(const rel_problem* p, const void* q, const 
                             {dv, tb, true, true, "dv"},
                             {dlambda, 4, false, true, "dlambda"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
 
   const int T = (int)p->T, D = (int)p->D;
   const size_t N = (size_t)(p->B * p->H);
@@ -998,7 +998,7 @@ rel_status relation_layer_fwd(const rel_problem* p, const rel_layer_opts* opts, 
                             {out, tb, true, true, "out"},
                             {row_stat, rb, false, true, "row_stat"},
                             {prep, L.prep, false, true, "saved / workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   const hipStream_t s = (hipStream_t)stream;
   const rel::LayerArgs a = layer_args(p, opts, L, prep, q, k, v, theta);
   const int vec = layer_vec(p, opts, {q, k, v, out});
@@ -1028,7 +1028,7 @@ rel_status relation_layer_bwd(const rel_problem* p, const rel_layer_opts* opts, 
   const hipStream_t s = (hipStream_t)stream;
   if (empty) {
     // nothing to differentiate: dlambda and dtheta are still outputs and must be zero
-    if (test_fail_launch() && (dlambda || (giv && dtheta))) return fail(REL_ERR_HIP, "launch failure injected");
+    if (test_fail_launch() && (dlambda || (giv && dtheta))) return fail(REL_ERR_HIP, "HIP launch failure injected");
     hipError_t e = hipSuccess;
     if (dlambda && (e = rel::launch_fill_zero(dlambda, 1, s))) return hip_fail(e, "dlambda clear");
     if (giv && dtheta && p->H > 0 && (e = rel::launch_fill_zero(dtheta, p->H / 2, s)))
@@ -1081,7 +1081,7 @@ rel_status relation_layer_bwd(const rel_problem* p, const rel_layer_opts* opts, 
                             {dlambda, 4, false, true, "dlambda"},
                             {giv ? dtheta : nullptr, thb, false, true, "dtheta"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::LayerArgs a = layer_args(p, opts, L, prep, q, k, v, theta);
   const int vec = layer_vec(p, opts, {q, k, v, out, dout, dq, dk, dv});
   hipError_t he = hipSuccess;
@@ -1179,7 +1179,7 @@ rel_status relation_decode_states(const rel_problem* p, const void* q, const voi
   if (nstates < 1 || nstates > 65535) return fail(REL_ERR_INVALID_ARG, "nstates must be in 1..65535");
   const size_t sb = (size_t)nstates * (size_t)(p->B * p->H) * (size_t)(p->D + 2) * 4;
   REL_TRY(check_decode_io(p, q, k_cache, v_cache, lengths, nullptr, nullptr, states, sb, true));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::DecodeArgs a = decode_args(p, q, k_cache, v_cache, lengths, nullptr);
   a.key0 = key_begin; a.key1 = key_end; a.nsplit = nstates; a.states = states;
   const hipError_t e = rel::launch_decode_states(a, p->dtype, (hipStream_t)stream);
@@ -1197,7 +1197,7 @@ rel_status relation_decode_merge(const rel_problem* p, int32_t nstates, const fl
   REL_TRY(check_aligned(lambda, 4, "lambda", true));
   const size_t sb = (size_t)nstates * (size_t)(p->B * p->H) * (size_t)(p->D + 2) * 4;
   REL_TRY(check_decode_io(p, q, k_cache, v_cache, lengths, out, row_stat, nstates ? states : nullptr, sb, false));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::DecodeArgs a = decode_args(p, q, k_cache, v_cache, lengths, lambda);
   a.nstates = nstates; a.states = (float*)states; a.out = out; a.row_stat = row_stat;
   const hipError_t e = rel::launch_decode_merge(a, p->dtype, (hipStream_t)stream);
@@ -1218,7 +1218,7 @@ rel_status relation_decode(const rel_problem* p, const void* q, const void* k_ca
   REL_TRY(check_aligned(workspace, 16, "workspace", true));
   REL_TRY(check_aligned(lambda, 4, "lambda", true));
   REL_TRY(check_decode_io(p, q, k_cache, v_cache, lengths, out, row_stat, (const float*)workspace, need, false));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::DecodeArgs a = decode_args(p, q, k_cache, v_cache, lengths, lambda);
   a.key0 = 0; a.key1 = (int)p->T; a.nsplit = decode_slices(p); a.states = (float*)workspace;
   a.nstates = a.nsplit; a.out = out; a.row_stat = row_stat;
@@ -1466,7 +1466,7 @@ static rel_status linear_fwd_impl(const rel_problem* p, const void* p1, const vo
                             {out, tb, true, true, "out"},
                             {state_out, N * (size_t)(p->D * p->D) * 4, false, true, "state_out"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::LinearArgs a{};
   a.p1 = p1; a.p2 = p2; a.v = v; a.g = g; a.out = out; a.state_out = state_out;
   a.a_log = a_log; a.dt_bias = dt_bias;
@@ -1552,7 +1552,7 @@ static rel_status linear_bwd_impl(const rel_problem* p, const void* p1, const vo
                             {da_log, pb, false, true, "da_log"},
                             {ddt_bias, pb, false, true, "ddt_bias"},
                             {workspace, need, false, true, "workspace"}}));
-  if (test_fail_launch()) return fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (test_fail_launch()) return fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   const LinearPlan L = linear_plan(p, linear_bf16(p, gated, rope_dim, true), true, gated, rope_dim);
   rel::LinearArgs a{};
   a.p1 = p1; a.p2 = p2; a.v = v; a.g = g; a.dy = dout;

@@ -169,7 +169,7 @@ rel_status relation_page_map(const rel_page_map* m, const int32_t* cached, const
                      {positions, N * 4, "positions", true},
                      {counts, 12, "counts", true}};
   REL_TRY(disjoint(r, 9));
-  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::PageMapArgs a{};
   a.cached = cached; a.added = added; a.free_pages = free_pages;
   a.table = table; a.lengths = lengths; a.row_start = row_start;
@@ -239,7 +239,7 @@ rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const 
   // the two caches may be interleaved in one allocation, as long as no element is shared
   const rel::ApiLattice L = {{c->stride_page, c->stride_head, c->stride_token}, {c->num_pages, c->H, c->page_size}, c->D};
   if (rel::api_alias(L, k_cache, v_cache, es)) return api_fail(REL_ERR_INVALID_ARG, "output k_cache overlaps v_cache");
-  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::AppendArgs a{};
   a.q = has_q ? q : nullptr; a.k = k; a.v = v;
   a.slots = slots; a.positions = positions; a.theta = theta;
@@ -302,7 +302,7 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
                      {row_stat, rows * 4, "row_stat", true},
                      {workspace, need, "workspace", true}};
   REL_TRY(disjoint(r, 9));
-  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   a.q = q; a.k = k_cache; a.v = v_cache; a.table = table; a.lengths = lengths; a.lambda = lambda;
   a.c = cache_of(c);
   a.B = (int)d->B; a.Hq = (int)d->Hq; a.W = (int)d->table_width;
@@ -363,7 +363,7 @@ rel_status relation_sample(const rel_sample* s, const void* logits, const float*
                      {logprob, B * 4, "logprob", true},
                      {workspace, need, "workspace", true}};
   REL_TRY(disjoint(r, 9));
-  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
   rel::SampleArgs a{};
   a.logits = logits; a.noise = noise;
   a.sl = s->B > 1 ? s->stride_logits : 0;

@@ -20,6 +20,13 @@ def lib():
     return R.load_library()
 
 
+@pytest.fixture(autouse=True)
+def _no_launch(monkeypatch):
+    """The addresses here are made up: a call whose arguments are accepted ends right before its launch, also where
+    there is a GPU."""
+    monkeypatch.setenv("RELATION_TEST_FAIL_LAUNCH", "1")
+
+
 def pages(P=10, page=16, H=2, D=64, dtype=R.REL_BF16, sp=None, sh=None, st=None):
     st = D if st is None else st
     sh = page * st if sh is None else sh
@@ -184,6 +191,24 @@ def test_injected_launch_failure(lib, monkeypatch):
     monkeypatch.setenv("RELATION_TEST_FAIL_LAUNCH", "1")
     for call in (page_map, append, decode, sample):
         assert call(lib) == HIP and b"injected" in lib.relation_last_error()
+
+
+def test_accepted_calls_end_before_the_launch(lib):
+    """What every other test here relies on, for each entry point."""
+    for call in (page_map, append, decode, sample):
+        assert call(lib) == HIP and b"injected" in lib.relation_last_error(), call.__name__
+
+
+def test_overlaps_are_named(lib):
+    for call, out, other in ((page_map, "counts", 0), (append, "qo", 1), (decode, "stat", 6), (sample, "lp", 6)):
+        assert call(lib, **{out: A[other]}) == BAD and b"overlaps" in lib.relation_last_error(), call.__name__
+
+
+def test_long_rows_need_a_workspace(lib):
+    """Rows over 8192 fp32 or 16384 bf16 logits take two kernels and a workspace between them."""
+    need = lambda V, dt: lib.relation_sample_workspace_bytes(ctypes.byref(R.RelSample(3, V, dt, V, V)))
+    for dt, most in ((R.REL_F32, 8192), (R.REL_BF16, 16384)):
+        assert need(most, dt) == 0 and need(most + 1, dt) > 0 and need(100000, dt) > 0
 
 
 def test_binding_refuses_what_is_not_on_the_gpu(lib):
