@@ -175,27 +175,39 @@ __device__ __forceinline__ void load_noise(const float* row, int V, const int (&
   }
 }
 
-// exp((x - top) / T) with log2(e) / T as hi + lo, so that the exponent keeps its fp32 accuracy however large.
+// exp((x - top) / T) with log2(e) / T as pre (hi + lo), so that the exponent keeps its fp32 accuracy however large.
+// pre is 1, or 2^24 for a T under 2^-126 whose log2(e) / T is past fp32.
 struct Scale {
-  float hi, lo;
+  float hi, lo, pre;
 };
+// A value that all lanes have, in a scalar register.
+__device__ __forceinline__ float scalar(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
 __device__ __forceinline__ Scale scale_of(float T) {
   const double c = 1.4426950408889634074 / (double)T;
-  Scale s;
-  s.hi = (float)c;
-  s.lo = s.hi < 3.0e38f ? (float)(c - (double)s.hi) : 0.0f;
-  return s;
+  const double d = c > 1.0e38 ? c * 0x1p-24 : c;
+  const float hi = (float)d;
+  return Scale{scalar(hi), scalar((float)(d - (double)hi)), scalar(c > 1.0e38 ? 0x1p24f : 1.0f)};
+}
+// (x - top) pre: with pre = 1 the difference, rounded once. From |top| = 2^100 on pre is left out, since top pre would
+// overflow: numbers there differ by 2^76 or not at all, and with such a T the exponent of a difference is out of range
+// either way.
+__device__ __forceinline__ float below_top(float x, float top, Scale s) {
+  const float pre = fabsf(top) < 0x1p100f ? s.pre : 1.0f;
+  return __builtin_fmaf(x, pre, -(top * pre));
 }
 __device__ __forceinline__ float weight(float x, float top, Scale s) {
-  const float t = x - top, y = t * s.hi;
+  const float t = below_top(x, top, s), y = t * s.hi;
   const float e = __builtin_fmaf(t, s.hi, -y) + t * s.lo, p = fast_exp2(y);
   // 1 for the largest, also where that is infinite; 0 for -inf, and where the exponent is past fp32's
   return x == top ? 1.0f : y > -150.0f ? __builtin_fmaf(p, e * kLn2, p) : 0.0f;
 }
 // The same to the rounding of the exponent (2^-23 of it, either way): for sums of
-// many. min and max pass over the NaN of inf - inf (1) and of 0 inf (0).
+// many. min and max pass over the NaN of inf - inf (1) and of inf - inf or 0 inf in the exponent (0: x is -inf or
+// below +inf).
 __device__ __forceinline__ float weight_fast(float x, float top, Scale s) {
-  const float t = fminf(x - top, 0.0f);
+  const float t = fminf(below_top(x, top, s), 0.0f);
   return fast_exp2(fmaxf(__builtin_fmaf(t, s.lo, t * s.hi), -1000.0f));
 }
 __device__ __forceinline__ float race(float w, float r) { return w / fmaxf(r, kTiny); }
@@ -584,7 +596,8 @@ __device__ __forceinline__ Round place_in_row(const TI* row, int V, int tid, con
     for (int s = 0; s < kAhead; ++s) {
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        const float y = element(u[s], e), t = fminf(y - top, 0.0f), w = fast_exp2(__builtin_fmaf(t, sc.lo, t * sc.hi));
+        const float y = element(u[s], e), t = fminf(below_top(y, top, sc), 0.0f),
+                    w = fast_exp2(__builtin_fmaf(t, sc.lo, t * sc.hi));
         const bool in = y > pivot.x;
         r.n += in;
         r.mass += in ? w : 0.0f;

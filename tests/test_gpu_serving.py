@@ -487,6 +487,31 @@ def test_sample_masks_and_infinities(V):
     assert bad["tokens"].tolist() == [-1] * 4 + [0] and torch.isnan(bad["logprob"][:4]).all()
 
 
+@pytest.mark.parametrize("V", [500, 40000])
+def test_sample_subnormal_temperatures(V):
+    """Temperatures under 2^-126: the largest logits share the weight, whatever their size, and logits that differ by
+    as little as the temperature keep their weights."""
+    rng = np.random.default_rng(28 + V)
+    tiny = float(np.float32(1e-40))
+    x = rng.standard_normal((9, V))
+    x[1] = 0.0
+    x[2, [7, 11, V - 1]] = 9.0
+    x[3] = -np.arange(V) * tiny           # weights exp(-0), exp(-1), exp(-2), ...
+    x[4] = -np.arange(V)[::-1] * tiny
+    x[5] = np.where(rng.random(V) < 0.5, 3.0e38, 2.9e38)
+    x[6, [3, V // 2]] = np.inf
+    x[7] = -np.inf
+    x[7, [5, 6]] = -1.0e38
+    x[8] = 1.0 + 2.0 ** -7 * rng.integers(0, 2, V)
+    r = _noise(9, V, rng)
+    for dtype in ("f32", "bf16"):
+        y = torch.from_numpy(x).to(torch.float32).to(TORCH_DT[dtype]).to(DEV)
+        log(f"[sample] subnormal T V={V} {dtype}")
+        for kw in (dict(T=1e-40), dict(T=4.2e-39, p=0.9), dict(T=1.5e-45, k=20, p=0.95), dict(T=1e-39, mp=0.1),
+                   dict(T=1e-38)):
+            _check_sample(y, r, **kw)
+
+
 def test_sample_strides_and_alignment():
     """Rows off 16-byte boundaries, rows apart from each other, rows read backwards from a transpose, no parameters."""
     rng = np.random.default_rng(24)
