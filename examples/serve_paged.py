@@ -65,7 +65,8 @@ class Pool:
     """The caches of all layers, the block tables of B requests, and the free pages."""
 
     def __init__(self, model, requests, pages, page_size, max_length, dev="cuda"):
-        shape = (model.layers, pages, 2, model.H, page_size, model.D)
+        width = -(-model.D // 8) * 8  # the caches' rows are multiples of 16 bytes; narrower heads are padded
+        shape = (model.layers, pages, 2, model.H, page_size, width)
         self.kv = torch.zeros(shape, dtype=torch.bfloat16, device=dev)
         self.table = torch.full((requests, -(-max_length // page_size)), -1, dtype=torch.int32, device=dev)
         self.free = torch.randperm(pages, device=dev).to(torch.int32)
@@ -127,8 +128,9 @@ def generate(model, prompts, steps, *, page_size=16, seed=1, **filters):
             q, k, v = model.qkv(n, x)
             q = R.relation_paged_append(k, v, *pool.caches(n), m["slots"], m["positions"], q=q, theta=model.theta[n],
                                         pairing=model.pairing[n])
-            o = R.relation_paged_decode(q, *pool.caches(n), pool.table, m["lengths"], model.lam[n], max_length=longest)["o"]
-            x = x + o.reshape(B, model.dim) @ model.wo[n]
+            o = R.relation_paged_decode(q, *pool.caches(n), pool.table, m["lengths"], model.lam[n], max_length=longest,
+                                        head_dim=model.D)["o"]
+            x = x + o[:, :, :model.D].reshape(B, model.dim) @ model.wo[n]
     return torch.stack(out, 1), torch.stack(logprob, 1), x
 
 

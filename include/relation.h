@@ -519,7 +519,8 @@ rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const 
  * infinite value in the history may come out as NaN in its channel. */
 typedef struct rel_paged_query {
   int64_t B, Hq, table_width, max_length;
-  float tau_s, scale; /* as in rel_problem; scale <= 0: 1/sqrt(c->D) */
+  float tau_s, scale; /* as in rel_problem; scale <= 0: 1/sqrt(c->D). Heads that relation_paged_append padded from D to
+                         c->D need their own scale here, 1/sqrt(D) by default elsewhere (relation_layer_fwd) */
 } rel_paged_query;
 size_t relation_paged_decode_workspace_bytes(const rel_pages* c, const rel_paged_query* d);
 rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, const void* q, const void* k_cache,

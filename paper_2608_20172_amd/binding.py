@@ -735,8 +735,9 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, theta=None,
                           pairing: Optional[str] = None, rope_base: float = ROPE_BASE, out=None):
     """New tokens' rows into the cache, in place: k (RoPE at the positions) and v (Givens mixing), [N, H, D], to
-    slots (int64 [N]) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc. With q [N, Hq, D], returns
-    the rotated and padded queries [N, Hq, Dc] (out["q"] where given), else None. rope_base 0 or None: no RoPE."""
+    slots (int64 [N]) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc (then relation_paged_decode
+    needs head_dim=D). With q [N, Hq, D], returns the rotated and padded queries [N, Hq, Dc] (out["q"] where given),
+    else None. rope_base 0 or None: no RoPE."""
     lib = load_library()
     dev = _on_gpu(k, v, k_cache, v_cache, slots, positions, q)
     c = make_pages(k_cache, v_cache)
@@ -779,10 +780,15 @@ def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, t
 
 
 def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_length: Optional[int] = None,
-                          tau_s: float = TAU_S, scale: Optional[float] = None, workspace=None, out=None):
+                          tau_s: float = TAU_S, scale: Optional[float] = None, head_dim: Optional[int] = None,
+                          workspace=None, out=None):
     """One decode step over pages: q [B, Hq, D] of the new tokens, caches [num_pages, H, page_size, D] (Hq a
     multiple of H), table int32 [B, W], lengths int32 [B] (the new token's own entry last), max_length a bound of
-    the lengths (default W * page_size). Returns dict(o [B, Hq, D], row_stat [B, Hq])."""
+    the lengths (default W * page_size). Returns dict(o [B, Hq, D], row_stat [B, Hq]).
+
+    The default scale is 1/sqrt(head_dim), and head_dim defaults to the caches' width D. Where relation_paged_append
+    padded narrower heads to D, the zeros change no product, but the scale is that of the true width: give it as
+    head_dim (or give scale), or the rows differ from relation_layer_fwd's."""
     lib = load_library()
     dev = _on_gpu(q, k_cache, v_cache, table, lengths)
     c = make_pages(k_cache, v_cache)
@@ -791,6 +797,12 @@ def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_lengt
     B, Hq, D = q.shape
     if table.dim() != 2 or table.shape[0] != B or lengths.shape != (B,):
         raise ValueError("table must be [B, W] and lengths [B]")
+    if head_dim is not None:
+        if scale is not None:
+            raise ValueError("give scale or head_dim, not both")
+        if not 1 <= head_dim <= D:
+            raise ValueError(f"head_dim must be in 1 .. the caches' width {D}")
+        scale = head_dim ** -0.5
     if not q.is_contiguous():
         q = q.contiguous()
     table, lengths = _ready(table, torch.int32), _ready(lengths, torch.int32)

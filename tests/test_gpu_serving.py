@@ -213,6 +213,41 @@ def test_paged_decode(lens, H, G, D, page, dtype, layout):
             assert torch.equal(r["o"][b], vc[table[b, 0], :, 0].repeat_interleave(G, 0))
 
 
+@pytest.mark.parametrize("D,Dc,dtype", [(60, 64, "bf16"), (48, 64, "bf16"), (80, 96, "bf16"), (60, 64, "f32"), (10, 12, "f32")])
+def test_padded_heads_decode_as_the_whole_sequence(D, Dc, dtype):
+    """Rows of a width that the cache pads, appended and decoded with the true width given: the last row of
+    relation_layer_fwd on the same heads, whose scale is 1/sqrt of the true width."""
+    rng = np.random.default_rng(51 + D)
+    T, H, page = 130, 4, 16
+    q, k, v = (torch.from_numpy(rng.standard_normal((T, H, D)) * 2.0).to(TORCH_DT[dtype]).to(DEV) for _ in range(3))
+    theta = torch.from_numpy(rng.uniform(-1, 1, H // 2)).float().to(DEV)
+    pages = -(-T // page)
+    kc, vc = (torch.zeros((pages, H, page, Dc), dtype=TORCH_DT[dtype], device=DEV) for _ in range(2))
+    table = _i32(rng.permutation(pages)[None])
+    m = R.relation_page_map(_i32([0]), _i32([T]), torch.zeros_like(table), table[0], page, T)
+    qr = R.relation_paged_append(k, v, kc, vc, m["slots"], m["positions"], q=q, theta=theta, pairing="A")
+    y = R.relation_paged_decode(qr[-1:], kc, vc, m["table"], m["lengths"], 0.5, head_dim=D)
+    torch.cuda.synchronize()
+    Y, M = SO.paged_decode(_np(qr[-1:]), _np(kc), _np(vc), _np(m["table"]).astype(int), [T], 0.5, scale=D ** -0.5)
+    _decode_close(y, Y, M, dtype)
+    w = R.relation_layer_fwd(*(t.transpose(0, 1)[None] for t in (q, k, v)), 0.5, theta, pairing="A")["o"][0, :, -1]
+    # bf16: both paths round q, k, v and y once each, and the whole sequence its weights: a few times 2^-8. fp32: the
+    # whole sequence's bar is 1e-4 of entries of some 0.3 and more, the decode step's 2e-5
+    err, bar = rel_l2(_np(y["o"][0, :, :D]), _np(w)), 2.0 ** -8 * 4 if dtype == "bf16" else 4e-4
+    log(f"[padded heads] D={D} Dc={Dc} {dtype}: {err:.2e} of the whole sequence's row (bar {bar:.1e})")
+    assert err <= bar and not y["o"][:, :, D:].any()
+
+
+def test_paged_decode_head_dim_is_checked():
+    kc, vc = _pool(2, 2, 16, 64, "bf16", "hnd", np.random.default_rng(53))
+    q, table, lens = kc[:1, :, 0].contiguous(), _i32([[0, 1]]), _i32([5])
+    for bad in (dict(head_dim=0), dict(head_dim=65), dict(head_dim=60, scale=0.1)):
+        with pytest.raises(ValueError, match="head_dim"):
+            R.relation_paged_decode(q, kc, vc, table, lens, 0.5, **bad)
+    a, b = (R.relation_paged_decode(q, kc, vc, table, lens, 0.5, **kw) for kw in (dict(head_dim=64), dict()))
+    assert torch.equal(a["o"], b["o"]) and torch.equal(a["row_stat"], b["row_stat"])
+
+
 @pytest.mark.parametrize("B,H,G,D,dtype", [(64, 3, 1, 48, "bf16"), (67, 2, 17, 80, "bf16"), (71, 3, 1, 40, "f32"),
                                            (65, 2, 6, 20, "f32")])
 def test_paged_decode_heads_that_share_lines(B, H, G, D, dtype):

@@ -43,3 +43,15 @@ def test_page_size_changes_nothing(model):
     prompts = _prompts(model, (5, 64))
     a, b = (E.generate(model, prompts, 12, page_size=p, temperature=0.0)[0] for p in (16, 64))
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("width", [60, 36])
+def test_heads_narrower_than_the_cache(width):
+    """Heads that the caches pad: the decode steps keep the scale of the true width."""
+    narrow = E.Decoder(vocab=3001, layers=2, heads=4, width=width)
+    prompts = _prompts(narrow, (1, 40, 200))
+    tokens, _, x = E.generate(narrow, prompts, 12, page_size=16, temperature=0.8, top_k=50)
+    torch.cuda.synchronize()
+    err = E.check(narrow, prompts, tokens, x)
+    print(f"width {width}: relative 2-norm {err:.2e} (bar {BAR:.2e})", flush=True)
+    assert err <= BAR
