@@ -678,6 +678,25 @@ def _ready(t: torch.Tensor, dtype) -> torch.Tensor:
     return t if t.dtype == dtype and t.is_contiguous() else t.detach().to(dtype).contiguous()
 
 
+INT32_MAX = 2 ** 31 - 1
+
+
+def _int32(t: torch.Tensor) -> torch.Tensor:
+    """``t`` in int32, contiguous: itself where it is. A number past 32 bits becomes the nearest that fits, which is out
+    of range for lengths, counts and page ids as the number itself is, and no bound for top_k; NaN becomes -1."""
+    if t.dtype == torch.int32:
+        return t if t.is_contiguous() else t.contiguous()
+    t = t.detach()
+    t = t.double().nan_to_num(nan=-1.0) if t.is_floating_point() else t.to(torch.int64)
+    return t.clamp(-INT32_MAX - 1, INT32_MAX).to(torch.int32).contiguous()
+
+
+def _positions(t: torch.Tensor) -> torch.Tensor:
+    """Positions in int32; one past 32 bits becomes -1, a token that is not written."""
+    p = _int32(t)
+    return p if t.dtype == torch.int32 else torch.where(t.detach() > INT32_MAX, -1, p)
+
+
 def make_pages(k_cache: torch.Tensor, v_cache: torch.Tensor) -> RelPages:
     """The pools [num_pages, H, page_size, D], with any strides that the library takes."""
     shape, strides, dt = k_cache.shape, k_cache.stride(), k_cache.dtype
@@ -706,7 +725,7 @@ def relation_page_map(cached, added, table, free_pages, page_size: int, max_toke
     B, W = table.shape
     if cached.shape != (B,) or added.shape != (B,) or free_pages.dim() != 1:
         raise ValueError("cached and added must be [B], free_pages [F]")
-    cached, added, free_pages = _ready(cached, i32), _ready(added, i32), _ready(free_pages, i32)
+    cached, added, free_pages = _int32(cached), _int32(added), _int32(free_pages)
     N = int(max_tokens)
     if N < 0:
         raise ValueError("max_tokens must not be negative")
@@ -755,7 +774,7 @@ def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, t
         v = _same_layout(k, v)[0]
     if slots.shape != (N,) or positions.shape != (N,):
         raise ValueError("slots and positions must be [N]")
-    slots, positions = _ready(slots, torch.int64), _ready(positions, torch.int32)
+    slots, positions = _ready(slots, torch.int64), _positions(positions)
     th = None if theta is None else _theta_tensor(theta, H, k.device)
     if givens and th is None:
         raise ValueError("theta is required for Givens mixing")
@@ -805,7 +824,7 @@ def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_lengt
         scale = head_dim ** -0.5
     if not q.is_contiguous():
         q = q.contiguous()
-    table, lengths = _ready(table, torch.int32), _ready(lengths, torch.int32)
+    table, lengths = _int32(table), _int32(lengths)
     lam_t = _lam_tensor(lam, q.device)
     d = RelPagedQuery(B, Hq, table.shape[1], int(max_length or 0), tau_s, 0.0 if scale is None else scale)
     o, rs = _given(out, "o", (B, Hq, D), q.dtype, dev), _given(out, "row_stat", (B, Hq), torch.float32, dev)
@@ -828,11 +847,13 @@ def _per_row(x, name, B, dtype, logits):
     if x is None:
         return None, None
     if not isinstance(x, torch.Tensor):
+        if dtype == torch.int32:
+            x = max(-1, min(x, INT32_MAX))
         x = logits.new_full((B,), x, dtype=dtype)
     elif x.shape != (B,) or x.get_device() != logits.get_device():
         raise ValueError(f"{name} must be a number, or [B] on the logits' GPU")
-    elif x.dtype != dtype or not x.is_contiguous():
-        x = x.detach().to(dtype).contiguous()
+    else:
+        x = _int32(x) if dtype == torch.int32 else _ready(x, dtype)
     return x.data_ptr(), x
 
 

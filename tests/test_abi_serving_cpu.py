@@ -211,6 +211,21 @@ def test_long_rows_need_a_workspace(lib):
         assert need(most, dt) == 0 and need(most + 1, dt) > 0 and need(100000, dt) > 0
 
 
+def test_whole_numbers_past_32_bits():
+    """They become the nearest number that fits, or no position; not the low half of their bits."""
+    far, top = 1 << 32, 2 ** 31 - 1
+    x = torch.tensor([far + 5, -far + 5, 7, top + 1, -1, 0])
+    assert R._int32(x).tolist() == [top, -top - 1, 7, top, -1, 0] and R._int32(x).dtype == torch.int32
+    assert R._positions(x).tolist() == [-1, -top - 1, 7, -1, -1, 0]
+    assert R._int32(torch.tensor([3e9, 5.0, float("nan"), float("inf")])).tolist() == [top, 5, -1, top]
+    assert R._int32(torch.tensor([200, 3], dtype=torch.uint8)).tolist() == [200, 3]
+    assert R._positions(torch.tensor([top], dtype=torch.int32)).tolist() == [top]
+    y = torch.arange(6, dtype=torch.int32)
+    assert R._int32(y) is y and R._int32(y[::2]).tolist() == [0, 2, 4] and R._int32(x.view(2, 3).t()).is_contiguous()
+    _, k = R._per_row(1 << 40, "top_k", 2, torch.int32, torch.zeros(2, 3))
+    assert k.tolist() == [top, top]
+
+
 def test_binding_refuses_what_is_not_on_the_gpu(lib):
     x = torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError, match="on the GPU"):

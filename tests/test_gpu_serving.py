@@ -364,6 +364,36 @@ def test_paged_offsets_past_32_bits():
     torch.cuda.empty_cache()
 
 
+def test_whole_numbers_past_32_bits_keep_their_meaning():
+    """int64 lengths, pages, counts and filters of 2^32 and more are out of range as they stand, not the small number
+    that their low half makes."""
+    i64 = lambda x: torch.tensor(x, dtype=torch.int64, device=DEV)
+    far = 1 << 32
+    m = R.relation_page_map(i64([far + 1, 0, 3]), i64([1, far + 2, -far + 1]), _i32([[5, 6], [-1, -1], [7, -1]]),
+                            i64([1, 2]), 4, 8)
+    assert m["counts"].tolist() == [0, 0, 3] and m["lengths"].tolist() == [0, 0, 0]
+    assert m["table"].tolist() == [[5, 6], [-1, -1], [7, -1]] and m["row_start"].tolist() == [0, 1, 8, 8]
+    m = R.relation_page_map(i64([0]), i64([1]), _i32([[-1]]), i64([far + 9]), 4, 1)
+    assert not 0 <= int(m["slots"][0]) // 4 < 1 << 28
+    rng = np.random.default_rng(41)
+    kc, vc = _pool(8, 2, 16, 64, "bf16", "hnd", rng)
+    q = torch.from_numpy(rng.standard_normal((3, 2, 64))).to(torch.bfloat16).to(DEV)
+    y = R.relation_paged_decode(q, kc, vc, i64([[1, 2], [3, far + 4], [5, 6]]), i64([20, 20, far + 20]), 0.5)
+    assert not torch.isnan(y["o"][0]).any() and torch.isnan(y["o"][1:]).all() and torch.isnan(y["row_stat"][1:]).all()
+    k = torch.from_numpy(rng.standard_normal((3, 2, 64))).to(torch.bfloat16).to(DEV)
+    before = kc.clone()
+    R.relation_paged_append(k, k, kc, vc, i64([0, 17, 35]), i64([far + 1, 4, -far + 1]), rope_base=None)
+    assert torch.equal(kc[1, :, 1], k[1])
+    kc[1, :, 1] = before[1, :, 1]
+    assert torch.equal(kc, before)
+    x = torch.zeros((2, 100), device=DEV)
+    x[:, 50] = 1.0
+    noise = torch.ones_like(x)
+    noise[:, 7] = 1e-6
+    t = R.relation_sample(x, noise, top_k=i64([far + 1, 1]))["tokens"]
+    assert t.tolist() == [7, 50]
+
+
 # ---------------------------------------------------------------------------
 # sampling
 # ---------------------------------------------------------------------------
