@@ -538,7 +538,7 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  * index), which is distributed as the kept w, renormalised, if noise holds
  * independent exponential variates (values below 2^-126 count as that).
  *   logits     [B, V] dtype, noise [B, V] fp32: element strides of the rows
- *              below, rows contiguous. noise is read for tokens in the running only.
+ *              below (0: one row for all, else at least V), rows contiguous. noise is read for tokens in the running only.
  *   temperature, top_p, min_p fp32 [B], top_k int32 [B]: NULL for 1, 1, 0, 0.
  *              T = 0 takes the first token (its logprob at T = 1).
  *   tokens     int64 [B]   logprob  fp32 [B], optional: d_i - ln Z of the token

@@ -321,8 +321,9 @@ static rel_status check_sample(const rel_sample* s, bool* empty) {
   if (s->V < 1) return api_fail(REL_ERR_INVALID_ARG, "a row without tokens");
   if (s->V > (1 << 22) || s->B > (1 << 20)) return api_fail(REL_ERR_UNSUPPORTED, "V is at most 2^22 and B at most 2^20");
   if (s->B * s->V > (1LL << 36)) return api_fail(REL_ERR_UNSUPPORTED, "B * V is over 2^36");
-  if (s->B > 1 && (s->stride_logits < s->V || s->stride_noise < s->V))
-    return api_fail(REL_ERR_INVALID_ARG, "row strides must be at least V");
+  // rows are only read: 0, one row for all, does no harm
+  if (s->B > 1 && ((s->stride_logits && s->stride_logits < s->V) || (s->stride_noise && s->stride_noise < s->V)))
+    return api_fail(REL_ERR_INVALID_ARG, "row strides must be 0 or at least V");
   if (s->B > 1 && (s->stride_logits > (1LL << 40) || s->stride_noise > (1LL << 40)))
     return api_fail(REL_ERR_UNSUPPORTED, "row stride over 2^40");
   return REL_OK;

@@ -193,6 +193,13 @@ def test_injected_launch_failure(lib, monkeypatch):
         assert call(lib) == HIP and b"injected" in lib.relation_last_error()
 
 
+def test_sample_row_strides(lib):
+    """0 is one row for all; rows are only read."""
+    assert sample(lib, sl=0) == HIP and sample(lib, sn=0) == HIP and sample(lib, sl=0, sn=0) == HIP
+    for bad in (-1000, -1, 1, 999):
+        assert sample(lib, sl=bad) == BAD and sample(lib, sn=bad) == BAD
+
+
 def test_accepted_calls_end_before_the_launch(lib):
     """What every other test here relies on, for each entry point."""
     for call in (page_map, append, decode, sample):

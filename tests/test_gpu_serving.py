@@ -577,6 +577,19 @@ def test_sample_subnormal_temperatures(V):
             _check_sample(y, r, **kw)
 
 
+def test_sample_several_tokens_from_one_row():
+    """Expanded logits (row stride 0) are read where they are, as their copies would be; expanded noise as well."""
+    rng = np.random.default_rng(29)
+    for V, dtype in ((1, "f32"), (300, "f32"), (20001, "bf16")):
+        x, r = _logits(1, V, dtype, rng), _noise(6, V, rng)
+        par = dict(temperature=0.9, top_k=40, top_p=0.95)
+        a, b = (R.relation_sample(y, r, **par) for y in (x.expand(6, V), x.expand(6, V).contiguous()))
+        assert torch.equal(a["tokens"], b["tokens"]) and torch.equal(a["logprob"], b["logprob"])
+        _check_sample(x.expand(6, V), r, T=0.9, k=40, p=0.95)
+        c = R.relation_sample(x.expand(6, V), r[:1].expand(6, V), **par)["tokens"]
+        assert c.tolist() == [int(c[0])] * 6
+
+
 def test_sample_strides_and_alignment():
     """Rows off 16-byte boundaries, rows apart from each other, rows read backwards from a transpose, no parameters."""
     rng = np.random.default_rng(24)
