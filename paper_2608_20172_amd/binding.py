@@ -771,6 +771,9 @@ def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, t
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("v must be as k")
     if v.stride() != ks:
+        if 0 in ks:  # expanded keys: no layout that the values could be copied to
+            k = k.contiguous()
+            ks = k.stride()
         v = _same_layout(k, v)[0]
     if slots.shape != (N,) or positions.shape != (N,):
         raise ValueError("slots and positions must be [N]")

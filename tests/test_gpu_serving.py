@@ -153,6 +153,20 @@ def test_append(N, H, Hq, D, Dc, page, dtype, layout, pairing, rope):
         assert got is None
 
 
+def test_append_expanded_rows():
+    """Keys of one head for all heads (stride 0) beside values of their own, and the other way round."""
+    rng = np.random.default_rng(44)
+    N, H, D, page = 5, 4, 64, 16
+    one, all_ = (torch.from_numpy(rng.standard_normal((N, h, D))).to(torch.bfloat16).to(DEV) for h in (1, H))
+    slots, positions = torch.arange(3, 3 + N, device=DEV), _i32(np.arange(N))
+    for k, v in ((one.expand(N, H, D), all_), (all_, one.expand(N, H, D)), (one.expand(N, H, D), one.expand(N, H, D)),
+                 (all_[:1].expand(N, H, D), all_)):
+        got, want = (_pool(2, H, page, D, "bf16", "hnd", np.random.default_rng(45)) for _ in range(2))
+        R.relation_paged_append(k, v, *got, slots, positions)
+        R.relation_paged_append(k.contiguous(), v.contiguous(), *want, slots, positions)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # ---------------------------------------------------------------------------
 # decode
 # ---------------------------------------------------------------------------
