@@ -181,8 +181,9 @@ struct Scale {
   float hi, lo, pre;
 };
 // A value that all lanes have, in a scalar register.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float scalar(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+  return __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, x)));
 }
 __device__ __forceinline__ Scale scale_of(float T) {
   const double c = 1.4426950408889634074 / (double)T;
@@ -512,10 +513,11 @@ struct Filters {
   float Z, bound, min_p;  // bound: top_p Z
   bool by_p;
   int k;
-  // whether token i is kept, by the tokens before it (min_p apart)
-  __device__ __forceinline__ bool kept(int i, const Round& before) const {
-    return i == top.i || (before.n < k && (!by_p || before.mass < bound));
+  // whether a token is kept by those before it (min_p apart); the first token is in any case
+  __device__ __forceinline__ bool within(const Round& before) const {
+    return before.n < k && (!by_p || before.mass < bound);
   }
+  __device__ __forceinline__ bool kept(int i, const Round& before) const { return i == top.i || within(before); }
 };
 __device__ __forceinline__ Filters filters_of(const RowParams& p, Best top, float Z) {
   return Filters{top, Z, p.top_p * Z, p.min_p, p.top_p < 1.0f, p.k};
@@ -636,6 +638,11 @@ __device__ __forceinline__ Round place_in_row(const TI* row, int V, int tid, con
   return r;
 }
 
+// Rounds over a row that pick runs before it looks for the filters' bound itself. Random numbers that know nothing of the
+// logits halve the tokens left in a round, about, and come to the end in a dozen; numbers that fall with the logits'
+// order take one token out a round, and there may be 2^22.
+constexpr int kRowRounds = 48;
+
 // Joins a row's chunks. `group` threads (a power of two) load a chunk's list,
 // kHeld tokens each at most, before it is known how long it is.
 template <typename TI>
@@ -725,7 +732,9 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
       if (tid < nch && mine.wi != 0x7fffffff)
         champion = Best{race(weight(mine.wx, top.v, sc), mine.wr), mine.wi, mine.wx};
       Best pivot = kNobody;
-      for (bool all = true;; all = false) {  // ends: fewer tokens race every time, and the first is always kept
+      bool bounded = false;  // the pivot is the first place whose token is not kept
+      for (int round = 0;; ++round) {
+        const bool all = round == 0;
         __syncthreads();
         for (int c = 0; c < nch; ++c) {
           if (!stale[c]) continue;
@@ -752,10 +761,45 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
         }
         Round r{champion, 0, 0.0f, 0.0f};
         pivot = reduce(r).win;
-        if (pivot.i == top.i) break;
-        r = place_in_row<TI>(row, a.V, tid, pivot, top.v, sc);
-        r = reduce(r);
-        if (f.kept(pivot.i, r) && weight(pivot.x, top.v, sc) >= p.min_p) break;
+        if (pivot.i == top.i || bounded) break;
+        // Is it kept? After kRowRounds, where is the first place whose token is not: by bisection of the logit (its
+        // ordered bits, from the pivot's to the first token's; is a token kept that has none of its equals before it?),
+        // then of the index among equals. At most 54 passes over the row.
+        Best at = pivot;
+        bool kept = false, searching = false;
+        unsigned lo = 0, hi = 0;
+        int i0 = 0, i1 = a.V;
+        for (;;) {
+          r = reduce(place_in_row<TI>(row, a.V, tid, at, top.v, sc));
+          const bool in = scalar((int)(f.within(r) && weight(at.x, top.v, sc) >= p.min_p));
+          if (!searching) {
+            kept = in;
+            if (kept || round < kRowRounds) break;
+            searching = true;
+            lo = scalar((int)ordered(pivot.x));
+            hi = scalar((int)ordered(top.v));
+            if (!f.within(Round{kNobody, 0, 0.0f, 0.0f}) || p.min_p > 1.0f) {  // the first token alone
+              lo = hi;
+              i0 = i1 = scalar(top.i) + 1;
+            }
+          } else if (lo < hi) {
+            if (in)
+              hi = lo + (hi - lo) / 2;
+            else
+              lo += (hi - lo) / 2 + 1;
+          } else if (in) {
+            i0 += (i1 - i0) / 2 + 1;
+          } else {
+            i1 = i0 + (i1 - i0) / 2;
+          }
+          if (lo >= hi && i0 >= i1) {  // the next round's winner is the token
+            pivot = Best{0.0f, i1, unordered(hi)};
+            bounded = true;
+            break;
+          }
+          at = Best{0.0f, lo < hi ? 0 : i0 + (i1 - i0) / 2, unordered(lo + (hi - lo) / 2)};
+        }
+        if (kept) break;
         if (tid < nch) stale[tid] = champion.i != 0x7fffffff && !stands_before(champion.x, champion.i, pivot);
       }
       token = pivot;

@@ -604,6 +604,41 @@ def test_sample_several_tokens_from_one_row():
         assert c.tolist() == [int(c[0])] * 6
 
 
+@pytest.mark.parametrize("V,dtype", [(9000, "f32"), (131072, "f32"), (131072, "bf16"), (1 << 20, "f32")])
+def test_sample_random_numbers_in_the_order_of_the_logits(V, dtype):
+    """Random numbers that fall along the order of the logits: the race's winner is always the last token left, and the
+    kept tokens are found all the same, in a time that the number of tokens does not multiply."""
+    # neighbours in the race are 3.6e-5 apart at least, and a level of 1000 gains more by them than it loses by its logit
+    step = np.arange(V) // 1000
+    x = np.zeros((8, V))
+    x[2:5] = -(2.0 ** -6) * step
+    x[5] = -(2.0 ** -6) * step[::-1]
+    x[6] = -np.arange(V) * 2.0 ** -18
+    x[7, V // 2:] = np.inf
+    w = np.exp(-(2.0 ** -6) * step)
+    before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+    at = 5432                                                          # kept by top-p: tokens 0 .. at
+    p = (before[at] + 0.5 * w[at]) / w.sum()
+    k = [V // 3, V - 1, 0, 0, 3500, 2999, V // 3, V // 5]
+    top_p = [1.0, 1.0, p, 1.0, 0.9999, 1.0, 1.0, 1.0]
+    min_p = [0.0, 0.0, 0.0, math.exp(-(2.0 ** -6) * 4.5), 0.0, 0.0, 0.0, 0.0]
+    y = torch.from_numpy(x).to(torch.float32).to(TORCH_DT[dtype]).to(DEV)
+    r = (3.0 * torch.exp(-4e-5 * torch.arange(V, dtype=torch.float64))).float().to(DEV).expand(8, V).contiguous()
+    r[5] = r[5].flip(0)
+    log(f"[sample] numbers in the logits' order V={V} {dtype}")
+    _check_sample(y, r, 1.0, k, top_p, min_p)
+    if V < 1 << 20:
+        _check_sample(y, r, 1.0, 0, 0.0, 0.0)
+        _check_sample(y, r, 1.0, 0, 1.0, 2.0)
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    R.relation_sample(y, r, top_k=_i32(k))
+    end.record()
+    torch.cuda.synchronize()
+    log(f"  {start.elapsed_time(end):.2f} ms")
+    assert start.elapsed_time(end) < 5.0 + V / 2000  # a round for each token left out would be over 0.02 V
+
+
 def test_sample_strides_and_alignment():
     """Rows off 16-byte boundaries, rows apart from each other, rows read backwards from a transpose, no parameters."""
     rng = np.random.default_rng(24)
