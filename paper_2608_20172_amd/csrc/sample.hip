@@ -639,9 +639,48 @@ __device__ __forceinline__ Round place_in_row(const TI* row, int V, int tid, con
 }
 
 // Rounds over a row that pick runs before it looks for the filters' bound itself. Random numbers that know nothing of the
-// logits halve the tokens left in a round, about, and come to the end in a dozen; numbers that fall with the logits'
+// logits halve the tokens left in a round, about, and come to the end in a dozen; numbers that fall along the logits'
 // order take one token out a round, and there may be 2^22.
 constexpr int kRowRounds = 48;
+
+// The winner among the kept tokens, given one that is not: the first place of the order whose token is not kept is found
+// by bisection, of the logit (its ordered bits, up to the first token's: is a token kept that has none of its equals
+// before it?), then of the index among equals. At most 55 passes over the row.
+template <typename TI, int NW>
+__device__ __forceinline__ Best race_bounded(const TI* row, const float* noise, int V, int tid, Best out, const RowParams& p,
+                                             Scale sc, const Filters& f, Reducer<NW>& reduce) {
+  unsigned lo = ordered(out.x), hi = ordered(f.top.v);
+  int i0 = 0, i1 = V;
+  if (!f.within(Round{kNobody, 0, 0.0f, 0.0f}) || p.min_p > 1.0f) return f.top;  // no other is kept
+  for (;;) {
+    const bool by_logit = lo < hi, found = !by_logit && i0 >= i1;
+    const unsigned u = lo + (hi - lo) / 2;
+    const int i = i0 + (i1 - i0) / 2;
+    const Best at{0.0f, by_logit ? 0 : found ? i1 : i, unordered(u)};
+    Round r{kNobody, 0, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int j = tid; j < V; j += kPickT) {
+      const float y = no_nan((float)row[j]);
+      if (!stands_before(y, j, at)) continue;
+      ++r.n;
+      r.mass += weight_fast(y, f.top.v, sc);
+      if (found) r.win = better(r.win, Best{race(weight(y, f.top.v, sc), noise[j]), j, y});
+    }
+    r = reduce(r);
+    if (found) return r.win;
+    const bool in = f.within(r) && weight(at.x, f.top.v, sc) >= p.min_p;
+    if (by_logit) {
+      if (in)
+        hi = u;
+      else
+        lo = u + 1;
+    } else if (in) {
+      i0 = i + 1;
+    } else {
+      i1 = i;
+    }
+  }
+}
 
 // Joins a row's chunks. `group` threads (a power of two) load a chunk's list,
 // kHeld tokens each at most, before it is known how long it is.
@@ -732,7 +771,6 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
       if (tid < nch && mine.wi != 0x7fffffff)
         champion = Best{race(weight(mine.wx, top.v, sc), mine.wr), mine.wi, mine.wx};
       Best pivot = kNobody;
-      bool bounded = false;  // the pivot is the first place whose token is not kept
       for (int round = 0;; ++round) {
         const bool all = round == 0;
         __syncthreads();
@@ -761,45 +799,14 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
         }
         Round r{champion, 0, 0.0f, 0.0f};
         pivot = reduce(r).win;
-        if (pivot.i == top.i || bounded) break;
-        // Is it kept? After kRowRounds, where is the first place whose token is not: by bisection of the logit (its
-        // ordered bits, from the pivot's to the first token's; is a token kept that has none of its equals before it?),
-        // then of the index among equals. At most 54 passes over the row.
-        Best at = pivot;
-        bool kept = false, searching = false;
-        unsigned lo = 0, hi = 0;
-        int i0 = 0, i1 = a.V;
-        for (;;) {
-          r = reduce(place_in_row<TI>(row, a.V, tid, at, top.v, sc));
-          const bool in = scalar((int)(f.within(r) && weight(at.x, top.v, sc) >= p.min_p));
-          if (!searching) {
-            kept = in;
-            if (kept || round < kRowRounds) break;
-            searching = true;
-            lo = scalar((int)ordered(pivot.x));
-            hi = scalar((int)ordered(top.v));
-            if (!f.within(Round{kNobody, 0, 0.0f, 0.0f}) || p.min_p > 1.0f) {  // the first token alone
-              lo = hi;
-              i0 = i1 = scalar(top.i) + 1;
-            }
-          } else if (lo < hi) {
-            if (in)
-              hi = lo + (hi - lo) / 2;
-            else
-              lo += (hi - lo) / 2 + 1;
-          } else if (in) {
-            i0 += (i1 - i0) / 2 + 1;
-          } else {
-            i1 = i0 + (i1 - i0) / 2;
-          }
-          if (lo >= hi && i0 >= i1) {  // the next round's winner is the token
-            pivot = Best{0.0f, i1, unordered(hi)};
-            bounded = true;
-            break;
-          }
-          at = Best{0.0f, lo < hi ? 0 : i0 + (i1 - i0) / 2, unordered(lo + (hi - lo) / 2)};
+        if (pivot.i == top.i) break;
+        r = place_in_row<TI>(row, a.V, tid, pivot, top.v, sc);
+        r = reduce(r);
+        if (f.kept(pivot.i, r) && weight(pivot.x, top.v, sc) >= p.min_p) break;
+        if (round == kRowRounds) {
+          pivot = race_bounded<TI>(row, noise, a.V, tid, pivot, p, sc, f, reduce);
+          break;
         }
-        if (kept) break;
         if (tid < nch) stale[tid] = champion.i != 0x7fffffff && !stands_before(champion.x, champion.i, pivot);
       }
       token = pivot;
