@@ -682,7 +682,7 @@ __device__ __forceinline__ Best race_bounded(const TI* row, const float* noise, 
   }
 }
 
-// Joins a row's chunks. `group` threads (a power of two) load a chunk's list,
+// Joins a row's chunks, at most one a thread. `group` threads (a power of two) load a chunk's list,
 // kHeld tokens each at most, before it is known how long it is.
 template <typename TI>
 __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int nch, int group, const Part* parts,
@@ -719,11 +719,6 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
   // the row's first token, the bound above which all tokens are listed, and whether a chunk has no list (n)
   Round r0{{mine.m, mine.mi, mine.m}, mine.n < 0, 0.0f, 0.0f};
   float tau = mine.tau;
-  for (int c = tid + kPickT; c < nch; c += kPickT) {
-    r0.win = better(r0.win, Best{parts[c].m, parts[c].mi, parts[c].m});
-    r0.n += parts[c].n < 0;
-    tau = fmaxf(tau, parts[c].tau);
-  }
   tau = wave_max(tau);
   if (lane == 0) taus[w] = tau;
   r0 = reduce(r0);
@@ -737,13 +732,10 @@ __global__ __launch_bounds__(kPickT) void sample_pick_kernel(SampleArgs a, int n
   // Z, and the winner of a race over all tokens
   Round r1{kNobody, 0, 0.0f, 0.0f};
   const bool race_all = !p.greedy && !p.filtered;
-  auto join = [&](const Part& q) {
-    if (q.m == kNegInf) return;
-    r1.z += q.z * weight(q.m, top.v, sc);
-    if (race_all && q.wi != 0x7fffffff) r1.win = better(r1.win, Best{race(weight(q.wx, top.v, sc), q.wr), q.wi, q.wx});
-  };
-  if (tid < nch) join(mine);
-  for (int c = tid + kPickT; c < nch; c += kPickT) join(parts[c]);
+  if (tid < nch && mine.m > kNegInf) {
+    r1.z = mine.z * weight(mine.m, top.v, sc);
+    if (race_all && mine.wi != 0x7fffffff) r1.win = Best{race(weight(mine.wx, top.v, sc), mine.wr), mine.wi, mine.wx};
+  }
   // the listed tokens that belong to the whole bound
   float v[kHeld];
   if (choose) {
@@ -1049,15 +1041,17 @@ __global__ __launch_bounds__(kRowT) void sample_row_kernel(SampleArgs a, int ran
 // these would be few, so that more of the chip reads (scan and pick together, fp32:
 // 1 row of 131072 15.7 us in 16 chunks, 13.5 in 64; 24 rows 18.6 and 18.0; 64 rows of
 // 32000, 256 chunks, 15.4 and 16.1).
+constexpr int kChunk = 8192, kFineChunk = 2048;
+static_assert(kSampleMaxV / kChunk <= kPickT, "a chunk a thread of pick");
 struct Cut {
   bool fine;
   int nch, rank, group, cap;
 };
 Cut cut_of(int64_t B, int64_t V) {
   Cut c;
-  const int64_t big = (V + 8191) / 8192;
-  c.fine = B * big < 256 && V <= 2048 * 256;
-  c.nch = (int)(c.fine ? (V + 2047) / 2048 : big);
+  const int64_t big = (V + kChunk - 1) / kChunk;
+  c.fine = B * big < 256 && V <= kFineChunk * 256;
+  c.nch = (int)(c.fine ? (V + kFineChunk - 1) / kFineChunk : big);
   c.rank = kTarget / (4 * c.nch);
   c.rank = c.rank < 1 ? 1 : c.rank > 40 ? 40 : c.rank;
   int pow2 = 1;

@@ -88,6 +88,7 @@ struct SampleArgs {
   int B, V;
   void* ws;
 };
+constexpr int64_t kSampleMaxV = 1 << 22;  // the largest row
 size_t sample_workspace_bytes(int64_t B, int64_t V, int dtype);
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream);
 

@@ -319,7 +319,7 @@ static rel_status check_sample(const rel_sample* s, bool* empty) {
   *empty = s->B == 0;
   if (*empty) return REL_OK;
   if (s->V < 1) return api_fail(REL_ERR_INVALID_ARG, "a row without tokens");
-  if (s->V > (1 << 22) || s->B > (1 << 20)) return api_fail(REL_ERR_UNSUPPORTED, "V is at most 2^22 and B at most 2^20");
+  if (s->V > rel::kSampleMaxV || s->B > (1 << 20)) return api_fail(REL_ERR_UNSUPPORTED, "V is at most 2^22 and B at most 2^20");
   if (s->B * s->V > (1LL << 36)) return api_fail(REL_ERR_UNSUPPORTED, "B * V is over 2^36");
   // rows are only read: 0, one row for all, does no harm
   if (s->B > 1 && ((s->stride_logits && s->stride_logits < s->V) || (s->stride_noise && s->stride_noise < s->V)))
