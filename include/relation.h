@@ -487,7 +487,8 @@ rel_status relation_page_map(const rel_page_map* m, const int32_t* cached, const
  *              element; 16-byte rows are fastest)
  *   slots      int64 [N]; positions int32 [N]. A token with a negative slot or
  *              position, or a slot past the pool, is not written and its q_out
- *              row is 0. Two tokens with one slot: either's row remains.
+ *              row is 0. The slots written in one call have to differ: of two
+ *              tokens with one slot, the row is left with parts of either.
  *   theta      fp32 [H/2] Givens angles (givens != NONE, H even)
  *   q_out      [N, Hq, c->D], dense, 16-byte aligned: rotated and padded
  *              queries, as relation_paged_decode takes them (with q)
@@ -516,7 +517,9 @@ rel_status relation_paged_append(const rel_pages* c, const rel_append* n, const 
  * workspace; <= 0 takes table_width * page_size. A request whose length is
  * outside 1 .. that bound, or one of whose pages is not in the pool, gets NaN
  * rows in out and row_stat. Entries past a request's length are not read. An
- * infinite value in the history may come out as NaN in its channel. */
+ * infinite value in the history may come out as NaN in its channel. B Hq rows of
+ * so many slices (of 128 to 4096 keys, by the number of rows) are refused over 2^22
+ * (REL_ERR_UNSUPPORTED); 2^14 rows of up to 2^20 tokens are not. */
 typedef struct rel_paged_query {
   int64_t B, Hq, table_width, max_length;
   float tau_s, scale; /* as in rel_problem; scale <= 0: 1/sqrt(c->D). Heads that relation_paged_append padded from D to
@@ -538,13 +541,14 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  * index), which is distributed as the kept w, renormalised, if noise holds
  * independent exponential variates (values below 2^-126 count as that).
  *   logits     [B, V] dtype, noise [B, V] fp32: element strides of the rows
- *              below (0: one row for all, else at least V), rows contiguous. noise is read for tokens in the running only.
+ *              below (0: one row for all, else at least V), rows contiguous.
+ *              Any entry of both may be read; the noise of tokens that are not kept changes nothing.
  *   temperature, top_p, min_p fp32 [B], top_k int32 [B]: NULL for 1, 1, 0, 0.
  *              T = 0 takes the first token (its logprob at T = 1).
  *   tokens     int64 [B]   logprob  fp32 [B], optional: d_i - ln Z of the token
  *              (before the filters)
  *   workspace  relation_sample_workspace_bytes(s) bytes, 16-byte aligned
- * NaN logits count as -inf; w is 0 at -inf, and below +inf, whatever T. A row with nothing above -inf, with a negative or
+ * NaN logits count as -inf; w is 0 at -inf, and below +inf, whatever T; a w under 2^-126 may count as 0. A row with nothing above -inf, with a negative or
  * NaN temperature or a NaN filter gives token -1 and logprob NaN.
  * V <= 2^22, B <= 2^20, B V <= 2^36. */
 typedef struct rel_sample {

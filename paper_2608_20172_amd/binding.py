@@ -754,9 +754,9 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 def relation_paged_append(k, v, k_cache, v_cache, slots, positions, *, q=None, theta=None,
                           pairing: Optional[str] = None, rope_base: float = ROPE_BASE, out=None):
     """New tokens' rows into the cache, in place: k (RoPE at the positions) and v (Givens mixing), [N, H, D], to
-    slots (int64 [N]) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc (then relation_paged_decode
-    needs head_dim=D). With q [N, Hq, D], returns the rotated and padded queries [N, Hq, Dc] (out["q"] where given),
-    else None. rope_base 0 or None: no RoPE."""
+    slots (int64 [N], those in use all different) of the caches [num_pages, H, page_size, Dc], zero-padded to Dc (then
+    relation_paged_decode needs head_dim=D). With q [N, Hq, D], returns the rotated and padded queries [N, Hq, Dc]
+    (out["q"] where given), else None. rope_base 0 or None: no RoPE."""
     lib = load_library()
     dev = _on_gpu(k, v, k_cache, v_cache, slots, positions, q)
     c = make_pages(k_cache, v_cache)
