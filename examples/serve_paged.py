@@ -78,9 +78,13 @@ class Pool:
         return self.kv[layer, :, 0], self.kv[layer, :, 1]
 
     def step(self, added):
-        """Pages and slots for added[b] more tokens of each request."""
+        """Pages and slots for added[b] more tokens of each request. Raises, and changes nothing, where they do not fit:
+        the map gives a request that it cannot serve length 0, and a loop that fed that back would start it over."""
         now = [c + a for c, a in zip(self.count, added)]
         need = sum(-(-n // self.page_size) + -c // self.page_size for n, c in zip(now, self.count))
+        if self.taken + need > len(self.free) or max(now) > self.table.shape[1] * self.page_size:
+            raise RuntimeError(f"{need} pages needed, {len(self.free) - self.taken} free; up to {max(now)} tokens of a "
+                               f"request, a table row holds {self.table.shape[1] * self.page_size}")
         m = R.relation_page_map(self.lengths, torch.tensor(added, dtype=torch.int32, device=self.table.device), self.table,
                                 self.free[self.taken:], self.page_size, sum(added))
         self.lengths, self.count, self.taken = m["lengths"], now, self.taken + need

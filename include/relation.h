@@ -457,7 +457,9 @@ typedef struct rel_pages {
  * free_pages, in the order of the list, requests in their order.
  *   table      in/out int32 [B, table_width]: entries have .. want - 1 of each
  *              served request are written, no others
- *   lengths    out int32 [B]: cached[b] + added[b]; 0 if not served
+ *   lengths    out int32 [B]: cached[b] + added[b]; 0 if not served. Such a
+ *              request still holds its cached[b] tokens: a caller that lets it
+ *              wait passes cached[b] again in the next step, not this 0
  *   row_start  out int32 [B + 1]: where the request's tokens stand among the
  *              step's, packed in the requests' order (sums of added[b], a
  *              negative one as 0), at most max_tokens

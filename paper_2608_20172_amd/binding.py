@@ -716,7 +716,9 @@ def relation_page_map(cached, added, table, free_pages, page_size: int, max_toke
     """Block tables, slots and positions of a step. cached, added: int32 [B]; table: int32 [B, W], updated in
     place; free_pages: int32 [F]; max_tokens: the step's token buffers. Returns dict(table, lengths [B],
     row_start [B + 1], slots int64 [max_tokens], positions [max_tokens], counts [3]: pages taken, tokens mapped,
-    requests not served), in the tensors of ``out`` where given."""
+    requests not served), in the tensors of ``out`` where given. A request that is not served has length 0 there and
+    keeps its place: where requests may wait for pages, the next step's cached is
+    torch.where(m["lengths"] > 0, m["lengths"], cached)."""
     lib = load_library()
     i32 = torch.int32
     dev = _on_gpu(table, cached, added, free_pages)

@@ -55,3 +55,27 @@ def test_heads_narrower_than_the_cache(width):
     err = E.check(narrow, prompts, tokens, x)
     print(f"width {width}: relative 2-norm {err:.2e} (bar {BAR:.2e})", flush=True)
     assert err <= BAR
+
+
+def test_a_step_that_does_not_fit_changes_nothing(model):
+    """The requests keep their places, and a smaller step goes on from them."""
+    pool = E.Pool(model, 2, 3, 16, 40)
+    pool.step([16, 15])
+    for added in ([17, 2], [0, 40]):  # two pages of the one left; a longer row than the table's
+        with pytest.raises(RuntimeError, match="pages needed"):
+            pool.step(added)
+        assert pool.lengths.tolist() == [16, 15] and pool.count == [16, 15] and pool.taken == 2
+    m = pool.step([3, 1])
+    assert m["lengths"].tolist() == [19, 16] and m["positions"].tolist() == [16, 17, 18, 15] and m["counts"].tolist() == [1, 4, 0]
+
+
+def test_a_request_that_waits_for_a_page_goes_on_from_its_place(model):
+    """The map alone, with the lengths of unserved requests kept as its documentation says."""
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    table, lengths = i32([[0, -1], [1, -1]]), i32([16, 16])
+    m = E.R.relation_page_map(lengths, i32([1, 1]), table, i32([2]), 16, 2)
+    assert m["lengths"].tolist() == [17, 0] and m["counts"].tolist() == [1, 1, 1]
+    lengths = torch.where(m["lengths"] > 0, m["lengths"], lengths)
+    m = E.R.relation_page_map(lengths, i32([1, 1]), table, i32([3]), 16, 2)
+    assert m["lengths"].tolist() == [18, 17] and m["positions"].tolist() == [17, 16]
+    assert m["slots"].tolist() == [2 * 16 + 1, 3 * 16] and table.tolist() == [[0, 2], [1, 3]]
