@@ -167,6 +167,15 @@ def test_append_expanded_rows():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("N,H,Hq,D,Dc,page,layout,pairing,rope", [
+    (5, 2, 2, 10, 16, 16, "hnd", "A", 1e4), (4100, 2, 1, 14, 16, 8, "nhd", "B", 1e4), (3, 3, 0, 2, 8, 4, "joint", None, 1e4),
+    (9, 2, 2, 7, 8, 16, "wide", "A", 0.0), (1, 1, 4, 1, 8, 1, "hnd", None, 0.0),
+])
+def test_append_narrow_rows(N, H, Hq, D, Dc, page, layout, pairing, rope):
+    """bf16 rows, or halves of them with RoPE, under 16 bytes."""
+    test_append(N, H, Hq, D, Dc, page, "bf16", layout, pairing, rope)
+
+
 # ---------------------------------------------------------------------------
 # decode
 # ---------------------------------------------------------------------------
@@ -283,6 +292,24 @@ def test_paged_decode_many_rows(B, H, G, D, top, page, dtype):
     log(f"[paged_decode] many rows B={B} H={H} G={G} D={D} up to {max(lens)} page={page} {dtype}")
     r, Y, M, _ = _decode_case(lens, H, G, D, page, dtype, "hnd")
     _decode_close(r, Y, M, dtype)
+
+
+@pytest.mark.parametrize("D,B,H", [(128, 50, 16), (32, 80, 10)])
+def test_paged_decode_long_slices_of_one_token_pages(D, B, H):
+    """Slices of 4096 pages of one token: the largest tables in LDS, beside the widest rows' tiles. The requests share
+    pages, and few of them are as long as the bound."""
+    rng = np.random.default_rng(62)
+    kc, vc = _pool(700, H, 1, D, "bf16", "hnd", rng)
+    W = 6000
+    table = rng.integers(0, 700, (B, W))
+    lens = np.where(np.arange(B) < 2, [W - b for b in range(B)], 1 + np.arange(B) * 7)
+    q = torch.from_numpy(rng.standard_normal((B, H, D))).to(torch.bfloat16).to(DEV)
+    log(f"[paged_decode] one-token pages D={D} B={B} H={H}")
+    r = R.relation_paged_decode(q, kc, vc, _i32(table), _i32(lens), 0.5)
+    torch.cuda.synchronize()
+    some = [0, 1, 2, B - 1]
+    Y, M = SO.paged_decode(_np(q[some]), _np(kc), _np(vc), table[some], lens[some], 0.5)
+    _decode_close({n: t[some] for n, t in r.items()}, Y, M, "bf16")
 
 
 def test_paged_decode_long():
@@ -668,6 +695,48 @@ def test_sample_frequencies():
     hits = np.bincount(t, minlength=V)
     assert hits.sum() == hits[kept].sum()
     assert np.all(np.abs(hits[kept] / n - w) < 5 * np.sqrt(w * (1 - w) / n))
+
+
+def test_outputs_and_workspaces_of_the_caller():
+    """out= and workspace= of append, decode and sample: the same values, in the caller's tensors; what does not fit is
+    refused."""
+    rng = np.random.default_rng(61)
+    B, H, D, page, W = 3, 2, 64, 16, 100
+    kc, vc = _pool(B * W, H, page, D, "bf16", "hnd", rng)
+    table = torch.arange(B * W, dtype=torch.int32, device=DEV).view(B, W)
+    lens = _i32([1600, 1, 900])
+    k = torch.from_numpy(rng.standard_normal((B, H, D))).to(torch.bfloat16).to(DEV)
+    slots = torch.tensor([1599, 1600, 3200 + 899], device=DEV)
+    want = R.relation_paged_append(k, k, kc, vc, slots, lens - 1, q=k)
+    out = {"q": torch.full_like(want, 9.0)}
+    assert R.relation_paged_append(k, k, kc, vc, slots, lens - 1, q=k, out=out) is out["q"] and torch.equal(out["q"], want)
+    y = R.relation_paged_decode(want, kc, vc, table, lens, 0.5)
+    c, d = R.make_pages(kc, vc), R.RelPagedQuery(B, H, W, 0, 2.0, 0.0)
+    need = R.load_library().relation_paged_decode_workspace_bytes(R.ctypes.byref(c), R.ctypes.byref(d))
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    out = {"o": torch.full_like(want, 9.0), "row_stat": torch.full((B, H), 9.0, device=DEV)}
+    got = R.relation_paged_decode(want, kc, vc, table, lens, 0.5, workspace=ws, out=out)
+    assert got["o"] is out["o"] and got["row_stat"] is out["row_stat"]
+    assert torch.equal(out["o"], y["o"]) and torch.equal(out["row_stat"], y["row_stat"])
+    x, r = _logits(B, 20000, "f32", rng), _noise(B, 20000, rng)
+    s = R.relation_sample(x, r, top_p=0.9)
+    need = R.load_library().relation_sample_workspace_bytes(R.ctypes.byref(R.RelSample(B, 20000, R.REL_F32, 20000, 20000)))
+    assert need > 0
+    sws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    out = {"tokens": torch.full((B,), 9, device=DEV), "logprob": torch.full((B,), 9.0, device=DEV)}
+    got = R.relation_sample(x, r, top_p=0.9, workspace=sws, out=out)
+    assert got["tokens"] is out["tokens"] and got["logprob"] is out["logprob"]
+    assert torch.equal(out["tokens"], s["tokens"]) and torch.equal(out["logprob"], s["logprob"])
+    small = torch.empty(16, dtype=torch.uint8, device=DEV)  # one that is too small is not used
+    assert torch.equal(R.relation_paged_decode(want, kc, vc, table, lens, 0.5, workspace=small)["o"], y["o"])
+    assert torch.equal(R.relation_sample(x, r, top_p=0.9, workspace=small)["tokens"], s["tokens"])
+    with pytest.raises(ValueError, match="contiguous"):
+        R.relation_paged_decode(want, kc, vc, table, lens, 0.5, out={"o": y["o"][:2]})
+    with pytest.raises(ValueError, match="contiguous"):
+        R.relation_sample(x, r, top_p=0.9, out={"tokens": s["tokens"].int()})
+    with pytest.raises(ValueError, match="contiguous"):
+        R.relation_paged_append(k, k, kc, vc, slots, lens - 1, q=k, out={"q": want.float()})
 
 
 # ---------------------------------------------------------------------------
