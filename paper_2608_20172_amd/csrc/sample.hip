@@ -638,7 +638,7 @@ __device__ __forceinline__ Round place_in_row(const TI* row, int V, int tid, con
   return r;
 }
 
-// Rounds over a row that pick runs before it looks for the filters' bound itself. Random numbers that know nothing of the
+// Rounds over a row before the filters' bound itself is looked for. Random numbers that know nothing of the
 // logits halve the tokens left in a round, about, and come to the end in a dozen; numbers that fall along the logits'
 // order take one token out a round, and there may be 2^22.
 constexpr int kRowRounds = 48;
@@ -646,7 +646,7 @@ constexpr int kRowRounds = 48;
 // The winner among the kept tokens, given one that is not: the first place of the order whose token is not kept is found
 // by bisection, of the logit (its ordered bits, up to the first token's: is a token kept that has none of its equals
 // before it?), then of the index among equals. At most 55 passes over the row.
-template <typename TI, int NW>
+template <typename TI, int NW>  // NW waves
 __device__ __forceinline__ Best race_bounded(const TI* row, const float* noise, int V, int tid, Best out, const RowParams& p,
                                              Scale sc, const Filters& f, Reducer<NW>& reduce) {
   unsigned lo = ordered(out.x), hi = ordered(f.top.v);
@@ -659,7 +659,7 @@ __device__ __forceinline__ Best race_bounded(const TI* row, const float* noise, 
     const Best at{0.0f, by_logit ? 0 : found ? i1 : i, unordered(u)};
     Round r{kNobody, 0, 0.0f, 0.0f};
 #pragma unroll 8
-    for (int j = tid; j < V; j += kPickT) {
+    for (int j = tid; j < V; j += NW * 64) {
       const float y = no_nan((float)row[j]);
       if (!stands_before(y, j, at)) continue;
       ++r.n;
@@ -989,7 +989,8 @@ __global__ __launch_bounds__(kRowT) void sample_row_kernel(SampleArgs a, int ran
     }
     if (!summed) f = filters_of(p, top, reduce(Round{kNobody, 0, 0.0f, z}).z);
     Best pivot = kNobody;
-    for (bool all = true; !p.greedy && !done; all = false) {  // ends: fewer tokens race every time, and the first is always kept
+    for (int round = 0; !p.greedy && !done; ++round) {
+      const bool all = round == 0;
       Round r{kNobody, 0, 0.0f, 0.0f};
       float near = -1.0f;  // what the approximations put below this does not win
       again();
@@ -1032,6 +1033,10 @@ __global__ __launch_bounds__(kRowT) void sample_row_kernel(SampleArgs a, int ran
         }
       }
       if (f.kept(pivot.i, reduce(r))) break;
+      if (round == kRowRounds) {
+        token = race_bounded<TI>(row, noise, a.V, tid, pivot, p, sc, f, reduce);
+        break;
+      }
     }
   }
   if (tid == 0) store_token(a, b, p, token, top.v, f.Z);

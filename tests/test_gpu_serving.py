@@ -631,7 +631,7 @@ def test_sample_several_tokens_from_one_row():
         assert c.tolist() == [int(c[0])] * 6
 
 
-@pytest.mark.parametrize("V,dtype", [(9000, "f32"), (131072, "f32"), (131072, "bf16"), (1 << 20, "f32")])
+@pytest.mark.parametrize("V,dtype", [(8192, "f32"), (16384, "bf16"), (9000, "f32"), (131072, "f32"), (131072, "bf16"), (1 << 20, "f32")])
 def test_sample_random_numbers_in_the_order_of_the_logits(V, dtype):
     """Random numbers that fall along the order of the logits: the race's winner is always the last token left, and the
     kept tokens are found all the same, in a time that the number of tokens does not multiply."""
