@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kMapT) void page_map_kernel(PageMapArgs a) {
 // Chunks are of 16 bytes whatever the width and the alignment: the last chunk of
 // a half is moved back to end with it, and repeats some channels of the one before
 // (the same values into the same places). 16384 tokens of 12 heads in bf16: width
-// 64 33 us (151 MB, 4.6 TB/s); width 60 in a cache of 64 51 us (147 MB), 64 with
+// 64 33 us (151 MB, 4.6 TB/s); width 60 in a cache of 64 51 us (146 MB), 64 with
 // 4-byte chunks, which divide a half of 30.
 // ---------------------------------------------------------------------------
 constexpr int kAppT = 256;
