@@ -431,8 +431,9 @@ rel_status relation_linear_gated_bwd(const rel_problem* p, const void* p1, const
  * page_size tokens; a request's block table names its pages in order. A step
  * of a serving loop is: relation_page_map (pages and slots of the step's
  * tokens), relation_paged_append (their rows into the pages),
- * relation_paged_decode (one new row per request and head), and, on the
- * model's logits, relation_sample. Lengths, page ids, slots and sampling
+ * relation_paged_decode (one new row per request and head) or
+ * relation_paged_prefill (any number of them), and, on the model's logits,
+ * relation_sample. Lengths, page ids, slots and sampling
  * parameters are device data that the host cannot check; the kernels read and
  * write only inside the buffers described here whatever they hold.
  *
@@ -532,6 +533,35 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
                                  const void* v_cache, const int32_t* table, const int32_t* lengths,
                                  const float* lambda, void* out, float* row_stat, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* A chunk of new tokens of each request over pages: the rows that
+ * relation_paged_decode would give one token at a time, for prompts (whole, in
+ * parts, or after a prefix that is in the cache already) and for steps where some
+ * requests add one token and others many. Request b's n_b = row_start[b + 1] -
+ * row_start[b] tokens stand in rows row_start[b] .. of q, as relation_page_map
+ * packs them, at the positions lengths[b] - n_b + 1 .. lengths[b]; their keys and
+ * values must be in the cache already. Row i is eqs. 1-3 at its position, over the
+ * request's entries 1 .. i.
+ *   q          [N, Hq, D] dense, 16-byte aligned   out  the same. Rows of no request
+ *              (before row_start[0], from row_start[B] on) are left as they are
+ *   table      int32 [B, table_width]; lengths int32 [B], this step's tokens
+ *              included; row_start int32 [B + 1], ascending, at most N
+ *   row_stat   fp32 [N, Hq], optional: M_i = ln Z_i + lambda ln i
+ *   workspace  relation_paged_prefill_workspace_bytes(c, d) bytes, 16-byte aligned
+ * max_length as in rel_paged_query. A request whose length is under n_b or over
+ * that bound gets NaN rows, and so does a row if a page of its entries is not in the
+ * pool. Entries past a request's length are not read; NaN and infinities in the
+ * entries after a row do not reach it. An infinite value among a row's own entries
+ * may come out as NaN in its channel. B at most 4096, N at most 2^26, N Hq at most 2^30. */
+typedef struct rel_paged_chunk {
+  int64_t N, B, Hq, table_width, max_length;
+  float tau_s, scale; /* as in rel_paged_query */
+} rel_paged_chunk;
+size_t relation_paged_prefill_workspace_bytes(const rel_pages* c, const rel_paged_chunk* d);
+rel_status relation_paged_prefill(const rel_pages* c, const rel_paged_chunk* d, const void* q, const void* k_cache,
+                                  const void* v_cache, const int32_t* table, const int32_t* lengths,
+                                  const int32_t* row_start, const float* lambda, void* out, float* row_stat,
+                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token of each row of logits. With d_i = (x_i - max x) / T, w_i = exp(d_i),
  * Z their sum, and the tokens in the order of falling x (equal ones: lower

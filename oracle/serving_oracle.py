@@ -17,7 +17,7 @@ from .decode_oracle import decode_step
 from .layer_oracle import givens
 from .relation_oracle import TAU_S
 
-__all__ = ["page_map", "turned", "append", "paged_decode", "sample"]
+__all__ = ["page_map", "turned", "append", "paged_decode", "paged_prefill", "sample"]
 
 
 def page_map(cached, added, table, free_pages, page_size: int, max_tokens: int) -> dict:
@@ -101,6 +101,34 @@ def paged_decode(q, k_cache, v_cache, table, lengths, lam, *, tau_s: float = TAU
             k = k_cache[ids, h * H // Hq].reshape(-1, D)[:n]
             v = v_cache[ids, h * H // Hq].reshape(-1, D)[:n]
             Y[b, h], M[b, h] = decode_step(q[b, h], k, v, n, lam, tau_s=tau_s, scale=scale)
+    return Y, M
+
+
+def paged_prefill(q, k_cache, v_cache, table, lengths, row_start, lam, *, tau_s: float = TAU_S, scale=None,
+                  max_length=None, rows=None):
+    """y [N, Hq, D] and M [N, Hq] of chunks of new tokens, a token at a time by `decode_step`; NaN for a request with a
+    bad length and for a row one of whose pages is bad. Rows of no request, and those not among `rows`, are None."""
+    P, H, page, D = k_cache.shape
+    N, Hq, _ = q.shape
+    W = np.shape(table)[1]
+    cap = min(W * page, max_length or W * page)
+    Y, M = [None] * N, [None] * N
+    for b in range(len(lengths)):
+        total, first, end = int(lengths[b]), int(row_start[b]), int(row_start[b + 1])
+        for r in range(first, end):
+            if rows is not None and r not in rows:
+                continue
+            n = total - (end - first) + (r - first) + 1  # its position, from 1
+            Y[r], M[r] = np.full((Hq, D), np.nan), np.full(Hq, np.nan)
+            if total < end - first or total > cap:
+                continue
+            ids = [int(x) for x in table[b][: -(-n // page)]]
+            if min(ids) < 0 or max(ids) >= P:
+                continue
+            for h in range(Hq):
+                k = k_cache[ids, h * H // Hq].reshape(-1, D)[:n]
+                v = v_cache[ids, h * H // Hq].reshape(-1, D)[:n]
+                Y[r][h], M[r][h] = decode_step(q[r, h], k, v, n, lam, tau_s=tau_s, scale=scale)
     return Y, M
 
 

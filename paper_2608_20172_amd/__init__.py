@@ -16,6 +16,7 @@ from .binding import (  # noqa: F401
     relation_page_map,
     relation_paged_append,
     relation_paged_decode,
+    relation_paged_prefill,
     relation_sample,
     load_library,
     TAU_S,

@@ -59,6 +59,11 @@ class RelPagedQuery(ctypes.Structure):
                 ("max_length", ctypes.c_int64), ("tau_s", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
+class RelPagedChunk(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("B", ctypes.c_int64), ("Hq", ctypes.c_int64), ("table_width", ctypes.c_int64),
+                ("max_length", ctypes.c_int64), ("tau_s", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
 class RelSample(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("V", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("stride_logits", ctypes.c_int64), ("stride_noise", ctypes.c_int64)]
@@ -116,6 +121,10 @@ _SIGS = {
                                                                 ctypes.POINTER(RelPagedQuery)]),
     "relation_paged_decode": (ctypes.c_int, [ctypes.POINTER(RelPages), ctypes.POINTER(RelPagedQuery)] + [_P] * 9 +
                               [ctypes.c_size_t, _P]),
+    "relation_paged_prefill_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelPages),
+                                                                 ctypes.POINTER(RelPagedChunk)]),
+    "relation_paged_prefill": (ctypes.c_int, [ctypes.POINTER(RelPages), ctypes.POINTER(RelPagedChunk)] + [_P] * 10 +
+                               [ctypes.c_size_t, _P]),
     "relation_sample_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelSample)]),
     "relation_sample": (ctypes.c_int, [ctypes.POINTER(RelSample)] + [_P] * 9 + [ctypes.c_size_t, _P]),
     "relation_profile_arm": (ctypes.c_int, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]),
@@ -844,6 +853,50 @@ def relation_paged_decode(q, k_cache, v_cache, table, lengths, lam, *, max_lengt
                                    o.data_ptr(), rs.data_ptr(), _ptr(ws), 0 if ws is None else _nbytes(ws), _stream_on(dev))
     if st:
         _check(st, "relation_paged_decode")
+    return {"o": o, "row_stat": rs}
+
+
+def relation_paged_prefill(q, k_cache, v_cache, table, lengths, row_start, lam, *, max_length: Optional[int] = None,
+                           tau_s: float = TAU_S, scale: Optional[float] = None, head_dim: Optional[int] = None,
+                           workspace=None, out=None):
+    """A chunk of new tokens of each request over pages: q [N, Hq, D], request b's tokens in rows row_start[b] ..
+    row_start[b + 1] - 1 (int32 [B + 1], as relation_page_map gives it), which are its last ones: positions up to
+    lengths[b] (int32 [B]), their keys and values in the caches [num_pages, H, page_size, D] already. table int32
+    [B, W]; max_length, scale, head_dim as for relation_paged_decode. Returns dict(o [N, Hq, D], row_stat [N, Hq]).
+    Rows of no request are not written: give ``out`` where they have to hold something."""
+    lib = load_library()
+    dev = _on_gpu(q, k_cache, v_cache, table, lengths, row_start)
+    c = make_pages(k_cache, v_cache)
+    if q.dim() != 3 or q.shape[2] != c.D or q.dtype != k_cache.dtype:
+        raise ValueError("q must be [N, Hq, D] with the caches' width and dtype")
+    N, Hq, D = q.shape
+    B = lengths.shape[0] if lengths.dim() == 1 else -1
+    if B < 0 or table.dim() != 2 or table.shape[0] != B or row_start.shape != (B + 1,):
+        raise ValueError("table must be [B, W], lengths [B] and row_start [B + 1]")
+    if head_dim is not None:
+        if scale is not None:
+            raise ValueError("give scale or head_dim, not both")
+        if not 1 <= head_dim <= D:
+            raise ValueError(f"head_dim must be in 1 .. the caches' width {D}")
+        scale = head_dim ** -0.5
+    if not q.is_contiguous():
+        q = q.contiguous()
+    table, lengths, row_start = _int32(table), _int32(lengths), _int32(row_start)
+    lam_t = _lam_tensor(lam, q.device)
+    d = RelPagedChunk(N, B, Hq, table.shape[1], int(max_length or 0), tau_s, 0.0 if scale is None else scale)
+    o, rs = _given(out, "o", (N, Hq, D), q.dtype, dev), _given(out, "row_stat", (N, Hq), torch.float32, dev)
+    if o is None:
+        o = torch.empty_like(q)
+    if rs is None:
+        rs = q.new_empty((N, Hq), dtype=torch.float32)
+    need = lib.relation_paged_prefill_workspace_bytes(ctypes.byref(c), ctypes.byref(d))
+    ws = _workspace(need, workspace, q.device) if need else None
+    st = lib.relation_paged_prefill(ctypes.byref(c), ctypes.byref(d), q.data_ptr(), k_cache.data_ptr(),
+                                    v_cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), row_start.data_ptr(),
+                                    lam_t.data_ptr(), o.data_ptr(), rs.data_ptr(), _ptr(ws),
+                                    0 if ws is None else _nbytes(ws), _stream_on(dev))
+    if st:
+        _check(st, "relation_paged_prefill")
     return {"o": o, "row_stat": rs}
 
 

@@ -1,5 +1,5 @@
 // Internal launch interface of the serving kernels: page maps, rows into a
-// paged cache, the decode step over pages, and sampling.
+// paged cache, the decode step and chunks of new tokens over pages, and sampling.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -74,6 +74,26 @@ struct PagedDecodeArgs {
 // Slices of a step: slice length and their number, by the host's bounds alone.
 void paged_decode_split(int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype, int* slice, int* nsplit);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, hipStream_t stream);
+
+struct PagedPrefillArgs {
+  const void* q;             // [N, Hq, D] dense
+  const void* k;
+  const void* v;
+  const int32_t* table;      // [B, W]
+  const int32_t* lengths;    // [B]
+  const int32_t* row_start;  // [B + 1]
+  const float* lambda;
+  PagedCache c;
+  int B, N, Hq, G, W;        // Hq = G * c.H
+  int max_len;               // lengths above it are refused (NaN)
+  float scale, inv_tau;
+  void* out;                 // [N, Hq, D] dense
+  float* row_stat;           // [N, Hq] or null
+  TileMap map;               // key heads x tiles (set by the launch)
+};
+// The largest batch: every workgroup finds its tile by a scan over the requests.
+constexpr int kPrefillMaxB = 4096;
+hipError_t launch_paged_prefill(const PagedPrefillArgs& a, int dtype, hipStream_t stream);
 
 struct SampleArgs {
   const void* logits;        // [B, V] with row stride `sl`

@@ -1,5 +1,5 @@
 // C-ABI layer of the serving entry points: page maps, rows into a paged cache,
-// the decode step over pages, and sampling. Arguments are checked on the host;
+// the decode step and chunks of new tokens over pages, and sampling. Arguments are checked on the host;
 // device data (lengths, page ids, slots) is checked where the kernels read it.
 #include "../../include/relation.h"
 
@@ -310,6 +310,73 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
   a.inv_tau = 1.0f / d->tau_s;
   a.states = (float*)workspace; a.out = out; a.row_stat = row_stat;
   return hip_status(rel::launch_paged_decode(a, c->dtype, (hipStream_t)stream), "paged decode launch");
+}
+
+// The step as a query of B requests, for the checks that the two share.
+static rel_status check_chunk(const rel_pages* c, const rel_paged_chunk* d, rel_paged_query* q, bool* empty) {
+  *q = rel_paged_query{};
+  if (d) *q = rel_paged_query{d->B, d->Hq, d->table_width, d->max_length, d->tau_s, d->scale};
+  REL_TRY(check_query(c, d ? q : nullptr, empty));
+  if (d->N < 0) return api_fail(REL_ERR_INVALID_ARG, "negative size of the query");
+  if (d->N == 0) *empty = true;
+  if (*empty) return REL_OK;
+  if (d->B > rel::kPrefillMaxB)
+    return api_fail(REL_ERR_UNSUPPORTED, "%lld requests: at most %d in one chunk step", (long long)d->B, rel::kPrefillMaxB);
+  if (d->N > (1 << 26) || d->N * d->Hq > (1 << 30)) return api_fail(REL_ERR_UNSUPPORTED, "over 2^26 tokens or 2^30 rows");
+  return REL_OK;
+}
+
+size_t relation_paged_prefill_workspace_bytes(const rel_pages* c, const rel_paged_chunk* d) {
+  bool empty = false;
+  rel_paged_query q;
+  if (check_chunk(c, d, &q, &empty) != REL_OK || empty) return 0;
+  return 0;
+}
+
+rel_status relation_paged_prefill(const rel_pages* c, const rel_paged_chunk* d, const void* q, const void* k_cache,
+                                  const void* v_cache, const int32_t* table, const int32_t* lengths,
+                                  const int32_t* row_start, const float* lambda, void* out, float* row_stat,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty = false;
+  rel_paged_query as_query;
+  REL_TRY(check_chunk(c, d, &as_query, &empty));
+  if (empty) return REL_OK;
+  const size_t need = relation_paged_prefill_workspace_bytes(c, d);
+  if (need && (!workspace || workspace_bytes < need))
+    return api_fail(REL_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+  REL_TRY(aligned(q, 16, "q"));
+  REL_TRY(aligned(k_cache, 16, "k_cache"));
+  REL_TRY(aligned(v_cache, 16, "v_cache"));
+  REL_TRY(aligned(table, 4, "table"));
+  REL_TRY(aligned(lengths, 4, "lengths"));
+  REL_TRY(aligned(row_start, 4, "row_start"));
+  REL_TRY(aligned(lambda, 4, "lambda"));
+  REL_TRY(aligned(out, 16, "out"));
+  REL_TRY(aligned(row_stat, 4, "row_stat", false));
+  REL_TRY(aligned(workspace, 16, "workspace", need > 0));
+  const size_t es = elem_size(c->dtype), pool = (size_t)pool_extent(c) * es;
+  const size_t rows = (size_t)(d->N * d->Hq);
+  const Range r[] = {{q, rows * (size_t)c->D * es, "q", false},
+                     {k_cache, pool, "k_cache", false},
+                     {v_cache, pool, "v_cache", false},
+                     {table, (size_t)(d->B * d->table_width) * 4, "table", false},
+                     {lengths, (size_t)d->B * 4, "lengths", false},
+                     {row_start, (size_t)(d->B + 1) * 4, "row_start", false},
+                     {lambda, 4, "lambda", false},
+                     {out, rows * (size_t)c->D * es, "out", true},
+                     {row_stat, rows * 4, "row_stat", true},
+                     {workspace, need, "workspace", true}};
+  REL_TRY(disjoint(r, 10));
+  if (rel::api_fail_launch()) return api_fail(REL_ERR_HIP, "HIP launch failure injected by RELATION_TEST_FAIL_LAUNCH");
+  rel::PagedPrefillArgs a{};
+  a.q = q; a.k = k_cache; a.v = v_cache; a.table = table; a.lengths = lengths; a.row_start = row_start; a.lambda = lambda;
+  a.c = cache_of(c);
+  a.B = (int)d->B; a.N = (int)d->N; a.Hq = (int)d->Hq; a.G = (int)(d->Hq / c->H); a.W = (int)d->table_width;
+  a.max_len = (int)longest(c, &as_query);
+  a.scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)c->D);
+  a.inv_tau = 1.0f / d->tau_s;
+  a.out = out; a.row_stat = row_stat;
+  return hip_status(rel::launch_paged_prefill(a, c->dtype, (hipStream_t)stream), "paged prefill launch");
 }
 
 static rel_status check_sample(const rel_sample* s, bool* empty) {
