@@ -593,6 +593,105 @@ rel_status relation_sample(const rel_sample* s, const void* logits, const float*
                            const int32_t* top_k, const float* top_p, const float* min_p, int64_t* tokens,
                            float* logprob, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Norms of query and key heads with the position rotation in the same pass, for
+ * training (before relation_fwd) and serving (before relation_paged_append with
+ * rope_base 0). Every row x [D] of a token and head becomes
+ *   n = x w / sqrt(mean(x^2) + eps)     (norm = 1; norm = 0: n = x)
+ *   channel pair j of the first rope_dim channels turned by the angle t w_j at the
+ *   token's position t: y_a = amplitude (n_a cos - n_b sin),
+ *   y_b = amplitude (n_a sin + n_b cos); the channels from rope_dim on are n.
+ * Pair j is (j, j + rope_dim/2) in layout REL_ROPE_HALF (as in relation_layer_fwd),
+ * (2j, 2j + 1) in REL_ROPE_INTERLEAVED. Frequencies: with
+ * v_j = rope_base^(-2j/rope_dim) and, for contexts longer than those trained on,
+ * a factor >= 1,
+ *   w_j = v_j (c_j + (1 - c_j) / factor),
+ *   c_j = clamp((original_length v_j / (2 pi) - low) / (high - low), 0, 1):
+ * pairs that turn `high` times or more within original_length keep their frequency,
+ * those that turn `low` times or less are slowed by the factor. original_length = 0
+ * slows them all (positions divided by the factor). factor = 1: w_j = v_j.
+ *   q [B,Hq,T,D], k [B,H,T,D] dtype; element strides per tensor, rows contiguous,
+ *              any alignment of the element (16-byte rows are fastest). Inputs may
+ *              have strides of 0, outputs not. Hq or H = 0: that tensor is absent.
+ *              Packed tokens [N, heads, D] are B = 1, T = N.
+ *   q_weight, k_weight  [D] in weight_dtype, shared by all heads; NULL: 1
+ *   positions  int32 [B, T] (rows contiguous, position_stride apart; 0: one row for
+ *              all); NULL: 0 .. T-1. A token at a negative position belongs to
+ *              nobody: its output rows are 0, and so are its gradients.
+ *   D <= 128; rope_dim even, 0 (no rotation) .. D; rope_base > 1.
+ * Angles are formed in 64 bits, sums in 32; each output is rounded once. NaN and
+ * infinities stay in their row (in the backward pass also in the weights' gradients). */
+typedef enum rel_rope_layout {
+  REL_ROPE_HALF = 0,
+  REL_ROPE_INTERLEAVED = 1
+} rel_rope_layout;
+typedef struct rel_strides {
+  int64_t b, h, t; /* elements */
+} rel_strides;
+typedef struct rel_qk_norm {
+  int64_t B, T, Hq, H, D;
+  rel_strides q, k;         /* the inputs */
+  rel_strides q_out, k_out; /* the outputs; backward: their gradients, which are read */
+  rel_strides dq, dk;       /* backward: the gradients written */
+  int64_t position_stride, rope_dim, original_length;
+  double rope_base, factor, low, high;
+  int32_t dtype, weight_dtype; /* rel_dtype */
+  int32_t norm, layout;        /* 0 or 1; rel_rope_layout */
+  float eps, amplitude;        /* eps > 0 (norm = 1) */
+} rel_qk_norm;
+rel_status relation_qk_norm_fwd(const rel_qk_norm* p, const void* q, const void* k, const void* q_weight,
+                                const void* k_weight, const int32_t* positions, void* q_out, void* k_out, void* stream);
+
+/* Backward: gradients of sum(dq_out * q_out) + sum(dk_out * k_out), recomputed from
+ * the inputs.
+ *   dq, dk     like q, k (strides of their own)
+ *   dq_weight, dk_weight  fp32 [D], optional (norm = 1): sums over tokens and heads
+ *              in a fixed order
+ *   workspace  relation_qk_norm_bwd_workspace_bytes(p) bytes, 16-byte aligned: the
+ *              weights' partial sums (needed with dq_weight or dk_weight) */
+size_t relation_qk_norm_bwd_workspace_bytes(const rel_qk_norm* p);
+rel_status relation_qk_norm_bwd(const rel_qk_norm* p, const void* q, const void* k, const void* q_weight,
+                                const void* k_weight, const int32_t* positions, const void* dq_out, const void* dk_out,
+                                void* dq, void* dk, float* dq_weight, float* dk_weight, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Log-probabilities of given tokens, with entropy, rank and the likeliest
+ * alternatives. With m = max x, Z = sum exp(x_i - m) and log p_i = x_i - m - ln Z
+ * over a row of logits:
+ *   logits     [N, V] dtype, element stride of the rows below (0: one row for all,
+ *              else at least V), rows contiguous
+ *   tokens     int64 [N]: the given token t of each row. Negative: the row has none
+ *              (logprob 0, rank -1, no gradient through logprob). From V on: logprob
+ *              NaN, rank -1, and a gradient of NaN
+ *   logprob    out fp32 [N], optional: log p_t
+ *   entropy    out fp32 [N], optional: -sum p_i log p_i
+ *   rank       out int32 [N], optional: tokens before t in the order of falling x
+ *              (equal ones: lower index first)
+ *   top_tokens, top_logprobs  out int64 and fp32 [N, K] (K > 0): the first K tokens
+ *              in that order and their log p
+ *   stats      out fp32 [N, 4], 16-byte aligned, optional: m, 1/Z, ln Z and the
+ *              entropy, for the backward pass
+ *   workspace  relation_token_logprobs_workspace_bytes(p) bytes, 16-byte aligned
+ * NaN logits count as -inf; p is 0 at -inf, and below +inf. A row with nothing above
+ * -inf has NaN in every fp32 output, rank -1 and top tokens -1.
+ * K <= 32, K <= V <= 2^22, N <= 2^20, N V <= 2^36.
+ * Backward: dlogits_i = g ([i = t] - p_i) - h p_i (log p_i + entropy), with
+ * g = dlogprob (fp32 [N]; NULL: 0), h = dentropy (the same). dlogits [N, V] dtype,
+ * rows stride_grad (at least V) elements apart. */
+typedef struct rel_token_logprobs {
+  int64_t N, V, K;
+  int32_t dtype;
+  int64_t stride_logits, stride_grad;
+} rel_token_logprobs;
+size_t relation_token_logprobs_workspace_bytes(const rel_token_logprobs* p);
+rel_status relation_token_logprobs_fwd(const rel_token_logprobs* p, const void* logits, const int64_t* tokens,
+                                       float* logprob, float* entropy, int32_t* rank, int64_t* top_tokens,
+                                       float* top_logprobs, float* stats, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+rel_status relation_token_logprobs_bwd(const rel_token_logprobs* p, const void* logits, const int64_t* tokens,
+                                       const float* stats, const float* dlogprob, const float* dentropy, void* dlogits,
+                                       void* stream);
+
 /* Measurement aid. While armed, every launch of the named kernel ("fwd": the
  * fused forward kernel; "bwd": all kernels of one relation_bwd call, back to
  * back; "bwd_dkdv": the dk/dv kernel, or the one-kernel backward's main

@@ -18,6 +18,12 @@ from .binding import (  # noqa: F401
     relation_paged_decode,
     relation_paged_prefill,
     relation_sample,
+    relation_qk_norm,
+    relation_qk_norm_fwd,
+    relation_qk_norm_bwd,
+    relation_token_logprobs,
+    relation_token_logprobs_fwd,
+    relation_token_logprobs_bwd,
     load_library,
     TAU_S,
 )

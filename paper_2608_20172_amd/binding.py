@@ -6,7 +6,8 @@ Functions carry the C-ABI names (relation_fwd, relation_bwd,
 relation_bwd_noalloc, relation_fwd_materialized, relation_bwd_materialized,
 relation_exchange_allocation, relation_layer_fwd, relation_layer_bwd,
 relation_decode, relation_decode_states, relation_decode_merge, ...). ``relation`` is the differentiable wrapper
-(torch.autograd.Function) over relation_fwd / relation_bwd.
+(torch.autograd.Function) over relation_fwd / relation_bwd, ``relation_qk_norm`` and
+``relation_token_logprobs`` those of the norms and of the log-probabilities.
 """
 from __future__ import annotations
 
@@ -69,6 +70,25 @@ class RelSample(ctypes.Structure):
                 ("stride_logits", ctypes.c_int64), ("stride_noise", ctypes.c_int64)]
 
 
+class RelStrides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
+
+
+class RelQkNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("B", "T", "Hq", "H", "D")] + \
+        [(n, RelStrides) for n in ("q", "k", "q_out", "k_out", "dq", "dk")] + \
+        [(n, ctypes.c_int64) for n in ("position_stride", "rope_dim", "original_length")] + \
+        [(n, ctypes.c_double) for n in ("rope_base", "factor", "low", "high")] + \
+        [(n, ctypes.c_int32) for n in ("dtype", "weight_dtype", "norm", "layout")] + \
+        [("eps", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class RelTokenLogprobs(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("stride_logits", ctypes.c_int64), ("stride_grad", ctypes.c_int64)]
+
+
+REL_ROPE = {"half": 0, "interleaved": 1}
 REL_GIVENS = {None: 0, "A": 1, "B": 2}
 REL_TRANSPORT = {"full": 0, "exchange": 1}
 ROPE_BASE = 1.0e4
@@ -127,6 +147,12 @@ _SIGS = {
                                [ctypes.c_size_t, _P]),
     "relation_sample_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelSample)]),
     "relation_sample": (ctypes.c_int, [ctypes.POINTER(RelSample)] + [_P] * 9 + [ctypes.c_size_t, _P]),
+    "relation_qk_norm_fwd": (ctypes.c_int, [ctypes.POINTER(RelQkNorm)] + [_P] * 8),
+    "relation_qk_norm_bwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelQkNorm)]),
+    "relation_qk_norm_bwd": (ctypes.c_int, [ctypes.POINTER(RelQkNorm)] + [_P] * 12 + [ctypes.c_size_t, _P]),
+    "relation_token_logprobs_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(RelTokenLogprobs)]),
+    "relation_token_logprobs_fwd": (ctypes.c_int, [ctypes.POINTER(RelTokenLogprobs)] + [_P] * 9 + [ctypes.c_size_t, _P]),
+    "relation_token_logprobs_bwd": (ctypes.c_int, [ctypes.POINTER(RelTokenLogprobs)] + [_P] * 7),
     "relation_profile_arm": (ctypes.c_int, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]),
     "relation_profile_disarm": (ctypes.c_int, []),
     "relation_mfma_peak_flops": (ctypes.c_int64, [ctypes.c_int, ctypes.c_int]),
@@ -949,6 +975,201 @@ def relation_sample(logits, noise, *, temperature=None, top_k=None, top_p=None, 
     return {"tokens": tokens, "logprob": logprob}
 
 
+# ---------------------------------------------------------------------------
+# Token by token: norms and rotation of heads, log-probabilities
+# ---------------------------------------------------------------------------
+def _head_strides(t: Optional[torch.Tensor]) -> RelStrides:
+    """(b, h, t) of [B, H, T, D], or of packed tokens [N, H, D] as B = 1."""
+    if t is None:
+        return RelStrides(0, 0, 0)
+    s = t.stride()
+    return RelStrides(s[0], s[1], s[2]) if t.dim() == 4 else RelStrides(0, s[1], s[0])
+
+
+def _head_rows(t: torch.Tensor) -> torch.Tensor:
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+def _dense_like(t: torch.Tensor) -> torch.Tensor:
+    """A dense tensor of t's shape with its order of heads and tokens: heads side by side as in a projection's output, or
+    a head's tokens one after another."""
+    if t.dim() == 4 and t.stride(2) >= t.stride(1) and t.shape[1] > 1:
+        B, H, T, D = t.shape
+        return t.new_empty((B, T, H, D)).transpose(1, 2)
+    return t.new_empty(t.shape)
+
+
+def _qk_norm_problem(q, k, q_weight, k_weight, positions, norm, eps, rope_dim, rope_base, layout, factor,
+                     original_length, low, high, amplitude):
+    """(problem, q, k, q_weight, k_weight, positions, device index); what is None stays None."""
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("q or k is needed")
+    dev = _on_gpu(one, q, k, q_weight, k_weight, positions)
+    if one.dim() not in (3, 4):
+        raise ValueError("q and k must be [B, H, T, D] or [N, H, D]")
+    heads = lambda t: (0 if t is None else t.shape[1])
+    if q is not None and k is not None and (q.dim() != k.dim() or q.dtype != k.dtype or
+                                            q.shape[:1] + q.shape[2:] != k.shape[:1] + k.shape[2:]):
+        raise ValueError("q and k must share all but their heads")
+    B, T = (one.shape[0], one.shape[2]) if one.dim() == 4 else (1, one.shape[0])
+    D = one.shape[-1]
+    if layout not in REL_ROPE:
+        raise ValueError("layout must be 'half' or 'interleaved'")
+    w = q_weight if q_weight is not None else k_weight
+    if w is not None:
+        if not norm:
+            raise ValueError("weights without a norm")
+        for x in (q_weight, k_weight):
+            if x is not None and (x.shape != (D,) or x.dtype != w.dtype or x.dtype not in (torch.float32, torch.bfloat16)):
+                raise ValueError("weights must be [D], both float32 or both bfloat16")
+    stride = 0
+    if positions is not None:
+        if positions.shape not in ((T,), (B, T)) or (one.dim() == 3 and positions.dim() != 1):
+            raise ValueError("positions must be [N] for packed tokens, else [T] or [B, T]")
+        if positions.dtype != torch.int32 or (T > 1 and positions.stride(-1) != 1) or \
+                (positions.dim() == 2 and B > 1 and 0 < positions.stride(0) < T):
+            positions = _positions(positions)
+        stride = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+    q, k = (None if t is None else _head_rows(t) for t in (q, k))
+    q_weight, k_weight = (None if x is None else x.contiguous() for x in (q_weight, k_weight))
+    p = RelQkNorm(B, T, heads(q), heads(k), D, _head_strides(q), _head_strides(k), RelStrides(), RelStrides(),
+                  RelStrides(), RelStrides(), stride, D if rope_dim is None else int(rope_dim), int(original_length),
+                  float(rope_base), float(factor), float(low), float(high), _dtype_code(one.dtype),
+                  REL_F32 if w is None else _dtype_code(w.dtype), int(bool(norm)), REL_ROPE[layout], float(eps),
+                  float(amplitude))
+    return p, q, k, q_weight, k_weight, positions, dev
+
+
+def _head_out(out, name, like, dev):
+    """out[name] where given (any strides over contiguous rows), else a dense tensor."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return _dense_like(like)
+    if t.shape != like.shape or t.dtype != like.dtype or t.get_device() != dev or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"out[{name!r}] must be like {name}, on GPU {dev}, with contiguous rows")
+    return t
+
+
+def relation_qk_norm_fwd(q, k, q_weight=None, k_weight=None, positions=None, *, norm: bool = True, eps: float = 1.0e-6,
+                         rope_dim: Optional[int] = None, rope_base: float = ROPE_BASE, layout: str = "half",
+                         factor: float = 1.0, original_length: int = 0, low: float = 1.0, high: float = 32.0,
+                         amplitude: float = 1.0, out=None):
+    """RMS norm of every head of q and k and the position rotation in one pass: q [B, Hq, T, D], k [B, H, T, D], or
+    packed tokens [N, heads, D] (either may be None); weights [D] or None. positions: int32 [T] or [B, T] ([N] for packed
+    tokens), None: 0 .. T-1; a token at a negative one gets zeros. rope_dim: the rotated channels (None: all, 0: none),
+    in pairs half a width apart or side by side (layout "half", "interleaved"); factor, original_length, low, high,
+    amplitude: longer contexts than those trained on (see relation.h). Returns dict(q, k), in the tensors of ``out``
+    where given."""
+    lib = load_library()
+    p, q, k, wq, wk, pos, dev = _qk_norm_problem(q, k, q_weight, k_weight, positions, norm, eps, rope_dim, rope_base,
+                                                 layout, factor, original_length, low, high, amplitude)
+    qo = None if q is None else _head_out(out, "q", q, dev)
+    ko = None if k is None else _head_out(out, "k", k, dev)
+    p.q_out, p.k_out = _head_strides(qo), _head_strides(ko)
+    st = lib.relation_qk_norm_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(wq), _ptr(wk), _ptr(pos), _ptr(qo), _ptr(ko),
+                                  _stream_on(dev))
+    if st:
+        _check(st, "relation_qk_norm_fwd")
+    return {"q": qo, "k": ko}
+
+
+def relation_qk_norm_bwd(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, *, norm: bool = True,
+                         eps: float = 1.0e-6, rope_dim: Optional[int] = None, rope_base: float = ROPE_BASE,
+                         layout: str = "half", factor: float = 1.0, original_length: int = 0, low: float = 1.0,
+                         high: float = 32.0, amplitude: float = 1.0, workspace=None, out=None):
+    """Gradients of relation_qk_norm_fwd from its inputs and those of its outputs. Returns dict(dq, dk, dwq, dwk (fp32
+    [D])); None for what is absent."""
+    lib = load_library()
+    p, q, k, wq, wk, pos, dev = _qk_norm_problem(q, k, q_weight, k_weight, positions, norm, eps, rope_dim, rope_base,
+                                                 layout, factor, original_length, low, high, amplitude)
+    grads = []
+    for name, x, g in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
+        if (x is None) != (g is None) or (x is not None and (g.shape != x.shape or g.dtype != x.dtype or g.get_device() != dev)):
+            raise ValueError(f"{name} must be like the output, on its GPU")
+        grads.append(None if g is None else _head_rows(g))
+    dqo, dko = grads
+    dq = None if q is None else _head_out(out, "dq", q, dev)
+    dk = None if k is None else _head_out(out, "dk", k, dev)
+    p.q_out, p.k_out, p.dq, p.dk = _head_strides(dqo), _head_strides(dko), _head_strides(dq), _head_strides(dk)
+    one = q if q is not None else k
+    dwq, dwk = (None if w is None else one.new_empty(p.D, dtype=torch.float32) for w in (wq, wk))
+    need = lib.relation_qk_norm_bwd_workspace_bytes(ctypes.byref(p)) if wq is not None or wk is not None else 0
+    ws = _workspace(need, workspace, one.device) if need else None
+    st = lib.relation_qk_norm_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(wq), _ptr(wk), _ptr(pos), _ptr(dqo), _ptr(dko),
+                                  _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(ws), _nbytes(ws), _stream_on(dev))
+    if st:
+        _check(st, "relation_qk_norm_bwd")
+    return {"dq": dq, "dk": dk, "dwq": dwq, "dwk": dwk}
+
+
+def relation_token_logprobs_fwd(logits, tokens, *, top: int = 0, want_rank: bool = False, workspace=None, out=None):
+    """Log-probabilities of the tokens (int64 [N]; negative: none given) under each row of logits [N, V]. Returns
+    dict(logprob, entropy (fp32 [N]), rank (int32 [N]: tokens before it, or None), top_tokens, top_logprobs (int64 and
+    fp32 [N, top]: the likeliest ones), stats (fp32 [N, 4], for the backward pass)), in the tensors of ``out`` where
+    given."""
+    lib = load_library()
+    dev = _on_gpu(logits, tokens)
+    if logits.dim() != 2 or tokens.shape != logits.shape[:1]:
+        raise ValueError("logits must be [N, V] and tokens [N]")
+    if tokens.is_floating_point() or tokens.dtype == torch.bool:
+        raise ValueError("tokens must be whole numbers")
+    N, V = logits.shape
+    sl, se = logits.stride()
+    if V > 1 and se != 1:
+        logits, sl = logits.contiguous(), V
+    tokens = _ready(tokens, torch.int64)
+    K = int(top)
+    p = RelTokenLogprobs(N, V, K, _dtype_code(logits.dtype), sl, 0)
+    f32 = torch.float32
+
+    def new(name, shape, dtype):
+        t = _given(out, name, shape, dtype, dev)
+        return logits.new_empty(shape, dtype=dtype) if t is None else t
+    logprob, entropy, stats = new("logprob", (N,), f32), new("entropy", (N,), f32), new("stats", (N, 4), f32)
+    rank = new("rank", (N,), torch.int32) if want_rank else None
+    tt, tl = new("top_tokens", (N, max(K, 0)), torch.int64), new("top_logprobs", (N, max(K, 0)), f32)
+    need = lib.relation_token_logprobs_workspace_bytes(ctypes.byref(p))
+    ws = _workspace(need, workspace, logits.device) if need else None
+    st = lib.relation_token_logprobs_fwd(ctypes.byref(p), logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(),
+                                         entropy.data_ptr(), _ptr(rank), tt.data_ptr(), tl.data_ptr(), stats.data_ptr(),
+                                         _ptr(ws), _nbytes(ws), _stream_on(dev))
+    if st:
+        _check(st, "relation_token_logprobs_fwd")
+    return {"logprob": logprob, "entropy": entropy, "rank": rank, "top_tokens": tt, "top_logprobs": tl, "stats": stats}
+
+
+def relation_token_logprobs_bwd(logits, tokens, stats, dlogprob=None, dentropy=None, *, out=None):
+    """The gradient by the logits of sum(dlogprob logprob) + sum(dentropy entropy), from the forward call's stats
+    (dlogprob, dentropy: fp32 [N] or None). Returns dlogits [N, V] (out["dlogits"] where given)."""
+    lib = load_library()
+    dev = _on_gpu(logits, tokens, stats, dlogprob, dentropy)
+    if logits.dim() != 2 or tokens.shape != logits.shape[:1]:
+        raise ValueError("logits must be [N, V] and tokens [N]")
+    N, V = logits.shape
+    if stats.shape != (N, 4) or stats.dtype != torch.float32:
+        raise ValueError("stats must be the forward call's")
+    for x in (dlogprob, dentropy):
+        if x is not None and x.shape != (N,):
+            raise ValueError("dlogprob and dentropy must be [N]")
+    sl, se = logits.stride()
+    if V > 1 and se != 1:
+        logits, sl = logits.contiguous(), V
+    tokens, stats = _ready(tokens, torch.int64), _ready(stats, torch.float32)
+    dlogprob, dentropy = (None if x is None else _ready(x, torch.float32) for x in (dlogprob, dentropy))
+    d = None if out is None else out.get("dlogits")
+    if d is None:
+        d = logits.new_empty((N, V))
+    elif d.shape != (N, V) or d.dtype != logits.dtype or d.get_device() != dev or (V > 1 and d.stride(1) != 1):
+        raise ValueError(f"out['dlogits'] must be like the logits, on GPU {dev}, with contiguous rows")
+    p = RelTokenLogprobs(N, V, 0, _dtype_code(logits.dtype), sl, d.stride(0))
+    st = lib.relation_token_logprobs_bwd(ctypes.byref(p), logits.data_ptr(), tokens.data_ptr(), stats.data_ptr(),
+                                         _ptr(dlogprob), _ptr(dentropy), d.data_ptr(), _stream_on(dev))
+    if st:
+        _check(st, "relation_token_logprobs_bwd")
+    return d
+
+
 def relation_profile_arm(kernel: str, events: list) -> None:
     """Record each listed torch.cuda.Event pair around successive launches of
     ``kernel`` ("fwd" or "bwd"); events = [start0, stop0, start1, stop1, ...]."""
@@ -987,3 +1208,46 @@ def relation(q, k, v, lam, tau_s: float = TAU_S, scale: Optional[float] = None) 
         lam = torch.tensor(float(lam), dtype=torch.float32, device=q.device)
     return _RelationFn.apply(q, k, v, lam, tau_s, scale)
 
+
+class _QkNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, opts):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        ctx.opts = opts
+        o = relation_qk_norm_fwd(q, k, q_weight, k_weight, positions, **opts)
+        return o["q"], o["k"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        g = relation_qk_norm_bwd(q, k, q_weight, k_weight, dq_out, dk_out, positions, **ctx.opts)
+        w = lambda d, x: None if x is None else d.to(x.dtype)
+        return g["dq"], g["dk"], w(g["dwq"], q_weight), w(g["dwk"], k_weight), None, None
+
+
+def relation_qk_norm(q, k, q_weight=None, k_weight=None, positions=None, **opts):
+    """Differentiable relation_qk_norm_fwd (its options): (q, k) normed and rotated, gradients for q, k and the weights."""
+    return _QkNormFn.apply(q, k, q_weight, k_weight, positions, opts)
+
+
+class _TokenLogprobsFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens):
+        f = relation_token_logprobs_fwd(logits, tokens)
+        ctx.save_for_backward(logits, tokens, f["stats"])
+        ctx.set_materialize_grads(False)
+        return f["logprob"], f["entropy"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogprob, dentropy):
+        logits, tokens, stats = ctx.saved_tensors
+        if dlogprob is None and dentropy is None:
+            return None, None
+        return relation_token_logprobs_bwd(logits, tokens, stats, dlogprob, dentropy), None
+
+
+def relation_token_logprobs(logits, tokens):
+    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]."""
+    return _TokenLogprobsFn.apply(logits, tokens)

@@ -20,8 +20,9 @@ BUILD_DIR = os.path.join(HERE, "_build")
 
 ARCH = "gfx950"
 SOURCES = ["fwd.hip", "bwd.hip", "rows.hip", "layer.hip", "decode.hip", "linear.hip", "linear_bf16.hip", "measure.hip",
-           "pages.hip", "paged_decode.hip", "paged_prefill.hip", "sample.hip", "relation_api.cpp", "serve_api.cpp"]
-API_SOURCES = ("relation_api.cpp", "serve_api.cpp")
+           "pages.hip", "paged_decode.hip", "paged_prefill.hip", "sample.hip", "qk_norm.hip",
+           "logprobs.hip", "relation_api.cpp", "serve_api.cpp", "token_api.cpp"]
+API_SOURCES = ("relation_api.cpp", "serve_api.cpp", "token_api.cpp")
 
 # Packed fp32 VALU instructions are disabled for all device code.
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
