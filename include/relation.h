@@ -671,7 +671,8 @@ rel_status relation_qk_norm_bwd(const rel_qk_norm* p, const void* q, const void*
  *              in that order and their log p
  *   stats      out fp32 [N, 4], 16-byte aligned, optional: m, 1/Z, ln Z and the
  *              entropy, for the backward pass
- *   workspace  relation_token_logprobs_workspace_bytes(p) bytes, 16-byte aligned
+ *   workspace  relation_token_logprobs_workspace_bytes(p) bytes, 16-byte aligned; it
+ *              serves fewer rows as well
  * NaN logits count as -inf; p is 0 at -inf, and below +inf. A row with nothing above
  * -inf has NaN in every fp32 output, rank -1 and top tokens -1.
  * K <= 32, K <= V <= 2^22, N <= 2^20, N V <= 2^36.

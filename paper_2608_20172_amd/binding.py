@@ -1121,14 +1121,18 @@ def relation_token_logprobs_fwd(logits, tokens, *, top: int = 0, want_rank: bool
     tokens = _ready(tokens, torch.int64)
     K = int(top)
     p = RelTokenLogprobs(N, V, K, _dtype_code(logits.dtype), sl, 0)
-    f32 = torch.float32
-
-    def new(name, shape, dtype):
-        t = _given(out, name, shape, dtype, dev)
-        return logits.new_empty(shape, dtype=dtype) if t is None else t
-    logprob, entropy, stats = new("logprob", (N,), f32), new("entropy", (N,), f32), new("stats", (N, 4), f32)
-    rank = new("rank", (N,), torch.int32) if want_rank else None
-    tt, tl = new("top_tokens", (N, max(K, 0)), torch.int64), new("top_logprobs", (N, max(K, 0)), f32)
+    f32, i32, i64, k = torch.float32, torch.int32, torch.int64, max(K, 0)
+    if out is None:  # one allocation for the fp32 outputs
+        stats, logprob, entropy, tl = logits.new_empty(N * (6 + k), dtype=f32).split_with_sizes((4 * N, N, N, k * N))
+        stats, tl, tt = stats.view(N, 4), tl.view(N, k), logits.new_empty((N, k), dtype=i64)
+        rank = logits.new_empty(N, dtype=i32) if want_rank else None
+    else:
+        def new(name, shape, dtype):
+            t = _given(out, name, shape, dtype, dev)
+            return logits.new_empty(shape, dtype=dtype) if t is None else t
+        logprob, entropy, stats = new("logprob", (N,), f32), new("entropy", (N,), f32), new("stats", (N, 4), f32)
+        rank = new("rank", (N,), i32) if want_rank else None
+        tt, tl = new("top_tokens", (N, k), i64), new("top_logprobs", (N, k), f32)
     need = lib.relation_token_logprobs_workspace_bytes(ctypes.byref(p))
     ws = _workspace(need, workspace, logits.device) if need else None
     st = lib.relation_token_logprobs_fwd(ctypes.byref(p), logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(),

@@ -257,7 +257,7 @@ rel_status relation_token_logprobs_fwd(const rel_token_logprobs* p, const void* 
   bool empty = false;
   REL_TRY(check_logprobs(p, false, &empty));
   if (empty) return REL_OK;
-  const size_t need = rel::logprobs_workspace_bytes(p->N, p->V, p->K, p->dtype);
+  const size_t need = rel::logprobs_scratch_bytes(p->N, p->V, p->K, p->dtype);
   if (need && (!workspace || workspace_bytes < need))
     return api_fail(REL_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
   const size_t es = elem_size(p->dtype), N = (size_t)p->N, K = (size_t)p->K;

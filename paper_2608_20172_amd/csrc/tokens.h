@@ -65,6 +65,8 @@ struct LogprobGradArgs {
 };
 constexpr int64_t kLogprobMaxV = 1 << 22;
 constexpr int kLogprobMaxK = 32;
+// Bytes that a call needs, and enough for every call of up to N rows.
+size_t logprobs_scratch_bytes(int64_t N, int64_t V, int64_t K, int dtype);
 size_t logprobs_workspace_bytes(int64_t N, int64_t V, int64_t K, int dtype);
 hipError_t launch_logprobs_fwd(const LogprobArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_logprobs_bwd(const LogprobGradArgs& a, int dtype, hipStream_t stream);
