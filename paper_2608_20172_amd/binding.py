@@ -1005,15 +1005,16 @@ def _qk_norm_problem(q, k, q_weight, k_weight, positions, norm, eps, rope_dim, r
     one = q if q is not None else k
     if one is None:
         raise ValueError("q or k is needed")
-    dev = _on_gpu(one, q, k, q_weight, k_weight, positions)
-    if one.dim() not in (3, 4):
+    dev = _on_gpu(one, k, q_weight, k_weight, positions)
+    shape = one.shape
+    nd = len(shape)
+    if nd not in (3, 4):
         raise ValueError("q and k must be [B, H, T, D] or [N, H, D]")
     heads = lambda t: (0 if t is None else t.shape[1])
-    if q is not None and k is not None and (q.dim() != k.dim() or q.dtype != k.dtype or
-                                            q.shape[:1] + q.shape[2:] != k.shape[:1] + k.shape[2:]):
+    if q is not None and k is not None and (k.dtype != q.dtype or k.dim() != nd or k.shape[0] != shape[0] or
+                                            k.shape[2:] != shape[2:]):
         raise ValueError("q and k must share all but their heads")
-    B, T = (one.shape[0], one.shape[2]) if one.dim() == 4 else (1, one.shape[0])
-    D = one.shape[-1]
+    (B, T, D) = (shape[0], shape[2], shape[3]) if nd == 4 else (1, shape[0], shape[2])
     if layout not in REL_ROPE:
         raise ValueError("layout must be 'half' or 'interleaved'")
     w = q_weight if q_weight is not None else k_weight
@@ -1025,14 +1026,16 @@ def _qk_norm_problem(q, k, q_weight, k_weight, positions, norm, eps, rope_dim, r
                 raise ValueError("weights must be [D], both float32 or both bfloat16")
     stride = 0
     if positions is not None:
-        if positions.shape not in ((T,), (B, T)) or (one.dim() == 3 and positions.dim() != 1):
+        pshape = positions.shape
+        if pshape != (T,) and (nd == 3 or pshape != (B, T)):
             raise ValueError("positions must be [N] for packed tokens, else [T] or [B, T]")
         if positions.dtype != torch.int32 or (T > 1 and positions.stride(-1) != 1) or \
-                (positions.dim() == 2 and B > 1 and 0 < positions.stride(0) < T):
+                (len(pshape) == 2 and B > 1 and 0 < positions.stride(0) < T):
             positions = _positions(positions)
-        stride = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+        if len(pshape) == 2 and B > 1:
+            stride = positions.stride(0)
     q, k = (None if t is None else _head_rows(t) for t in (q, k))
-    q_weight, k_weight = (None if x is None else x.contiguous() for x in (q_weight, k_weight))
+    q_weight, k_weight = (x if x is None or x.is_contiguous() else x.contiguous() for x in (q_weight, k_weight))
     p = RelQkNorm(B, T, heads(q), heads(k), D, _head_strides(q), _head_strides(k), RelStrides(), RelStrides(),
                   RelStrides(), RelStrides(), stride, D if rope_dim is None else int(rope_dim), int(original_length),
                   float(rope_base), float(factor), float(low), float(high), _dtype_code(one.dtype),

@@ -11,8 +11,14 @@
 // members of a pair meet in one lane, the row's sum is one reduction over the
 // group, and every channel is read and written once, in pieces of up to 16 bytes on
 // any boundary. Cosines and sines of a workgroup's tokens go to LDS once, for all
-// heads (the angle in 64-bit turns, so that a long context keeps its fraction).
-// Bound by memory.
+// heads of a tensor (the angle in 64-bit turns, so that a long context keeps its
+// fraction), while the first rows are read.
+// Bound by memory. 8 x 2048 tokens, 24 heads x 64 in bf16: forward (101 MB) 24 us, 4.2
+// TB/s, backward (151 MB) 34, 4.5; 16384 x 20 heads x 128 36 and 53; fp32, 4 x 4096 x 16 x
+// 64 24 (5.7 TB/s) and 38. 8 tokens a workgroup 26 and 42 of the first. One workgroup for
+// both tensors, without rows read ahead, 25 and 59: the sums for both weights take 32
+// registers, and rows came one after another. Widths whose runs are not whole pieces
+// of 16 bytes pay for it: 60 (pieces of 4 bytes) 2.2 TB/s, 80 (five of eight lanes) 3.2.
 #include <type_traits>
 
 #include "lanes.h"
@@ -23,65 +29,72 @@ namespace rel {
 namespace {
 
 constexpr int kT = 256;
-constexpr int kMaxTokens = 8;     // tokens of a workgroup at a time
-constexpr int kMaxGroups = 1024;  // workgroups of the backward pass
+constexpr int kMaxTokens = 16;   // tokens of a workgroup at a time
+constexpr int kMaxGroups = 512;  // workgroups of the backward pass a tensor: the two fill the chip once
 
-// N elements (of 2 to 16 bytes in all) on any element boundary, as floats.
+// N elements (2 to 16 bytes) on any element boundary: as they are read, so that loads are in flight together, and as
+// floats.
 template <typename TI, int N>
-struct Piece {
-  typedef TI V __attribute__((ext_vector_type(N), aligned(sizeof(TI))));
-};
-template <typename TI, int N>
-__device__ __forceinline__ void load_piece(const TI* p, float (&x)[N]) {
-  if constexpr (N == 1) {
-    x[0] = (float)*p;
-  } else if constexpr (sizeof(TI) == 4) {
-    const typename Piece<float, N>::V u = *reinterpret_cast<const typename Piece<float, N>::V*>(p);
+struct Piece;
+template <int N>
+struct Piece<float, N> {
+  typedef float V __attribute__((ext_vector_type(N), aligned(4)));
+  static __device__ __forceinline__ void values(const V& u, float* x) {
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = u[e];
-  } else {
-    typedef unsigned int U __attribute__((ext_vector_type(N / 2), aligned(2)));
-    if constexpr (N == 2) {
-      typedef unsigned int W __attribute__((aligned(2)));
-      const unsigned int u = *reinterpret_cast<const W*>(p);
-      x[0] = bf16_lo(u);
-      x[1] = bf16_hi(u);
-    } else {
-      const U u = *reinterpret_cast<const U*>(p);
-#pragma unroll
-      for (int e = 0; e < N / 2; ++e) {
-        x[2 * e] = bf16_lo(u[e]);
-        x[2 * e + 1] = bf16_hi(u[e]);
-      }
-    }
   }
-}
-template <typename TI, int N>
-__device__ __forceinline__ void store_piece(TI* p, const float (&x)[N]) {
-  if constexpr (N == 1) {
-    *p = (TI)x[0];
-  } else if constexpr (sizeof(TI) == 4) {
-    typename Piece<float, N>::V u;
+  static __device__ __forceinline__ V from(const float* x) {
+    V u;
 #pragma unroll
     for (int e = 0; e < N; ++e) u[e] = x[e];
-    *reinterpret_cast<typename Piece<float, N>::V*>(p) = u;
-  } else {
+    return u;
+  }
+};
+template <>
+struct Piece<float, 1> {
+  typedef float V;
+  static __device__ __forceinline__ void values(const V& u, float* x) { x[0] = u; }
+  static __device__ __forceinline__ V from(const float* x) { return x[0]; }
+};
+template <int N>
+struct Piece<bf16, N> {
+  typedef unsigned int V __attribute__((ext_vector_type(N / 2), aligned(2)));
+  static __device__ __forceinline__ void values(const V& u, float* x) {
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+      x[2 * e] = bf16_lo(u[e]);
+      x[2 * e + 1] = bf16_hi(u[e]);
+    }
+  }
+  static __device__ __forceinline__ V from(const float* x) {
     typedef __bf16 B __attribute__((ext_vector_type(N)));
     typedef float F __attribute__((ext_vector_type(N)));
+    typedef unsigned int U __attribute__((ext_vector_type(N / 2)));
     F f;
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] = x[e];
-    const B b = __builtin_convertvector(f, B);
-    if constexpr (N == 2) {
-      typedef unsigned int W __attribute__((aligned(2)));
-      *reinterpret_cast<W*>(p) = __builtin_bit_cast(unsigned int, b);
-    } else {
-      typedef unsigned int U __attribute__((ext_vector_type(N / 2), aligned(2)));
-      typedef unsigned int UA __attribute__((ext_vector_type(N / 2)));
-      *reinterpret_cast<U*>(p) = __builtin_bit_cast(UA, b);
-    }
+    return __builtin_bit_cast(U, __builtin_convertvector(f, B));
   }
-}
+};
+template <>
+struct Piece<bf16, 2> {
+  typedef unsigned int V __attribute__((aligned(2)));
+  static __device__ __forceinline__ void values(const V& u, float* x) {
+    x[0] = bf16_lo(u);
+    x[1] = bf16_hi(u);
+  }
+  static __device__ __forceinline__ V from(const float* x) {
+    typedef __bf16 B __attribute__((ext_vector_type(2)));
+    typedef float F __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned int, __builtin_convertvector(F{x[0], x[1]}, B));
+  }
+};
+template <>
+struct Piece<bf16, 1> {
+  typedef bf16 V;
+  static __device__ __forceinline__ void values(const V& u, float* x) { x[0] = (float)u; }
+  static __device__ __forceinline__ V from(const float* x) { return (bf16)x[0]; }
+};
 
 // Unit u of a row: the first channels of its two runs, and what they are.
 struct Unit {
@@ -108,29 +121,24 @@ __device__ __forceinline__ Unit unit_of(const QkNormArgs& a, int u) {
   return x;
 }
 
+// A unit of a row, as it is read.
 template <typename TI, int V>
-__device__ __forceinline__ void load_unit(const TI* row, const Unit& u, float (&x)[2 * V]) {
-  float p[V], q[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) p[e] = q[e] = 0.0f;
-  if (u.some) load_piece<TI, V>(row + u.a, p);
-  if (u.both) load_piece<TI, V>(row + u.b, q);
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    x[e] = p[e];
-    x[V + e] = q[e];
+struct RawUnit {
+  typename Piece<TI, V>::V p, q;
+  __device__ __forceinline__ void load(const TI* row, const Unit& u) {
+    p = q = typename Piece<TI, V>::V{};
+    if (u.some) p = *reinterpret_cast<const typename Piece<TI, V>::V*>(row + u.a);
+    if (u.both) q = *reinterpret_cast<const typename Piece<TI, V>::V*>(row + u.b);
   }
-}
+  __device__ __forceinline__ void values(float (&x)[2 * V]) const {
+    Piece<TI, V>::values(p, x);
+    Piece<TI, V>::values(q, x + V);
+  }
+};
 template <typename TI, int V>
 __device__ __forceinline__ void store_unit(TI* row, const Unit& u, const float (&x)[2 * V]) {
-  float p[V], q[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    p[e] = x[e];
-    q[e] = x[V + e];
-  }
-  if (u.some) store_piece<TI, V>(row + u.a, p);
-  if (u.both) store_piece<TI, V>(row + u.b, q);
+  if (u.some) *reinterpret_cast<typename Piece<TI, V>::V*>(row + u.a) = Piece<TI, V>::from(x);
+  if (u.both) *reinterpret_cast<typename Piece<TI, V>::V*>(row + u.b) = Piece<TI, V>::from(x + V);
 }
 template <int V>
 __device__ __forceinline__ void load_weights(const QkNormArgs& a, const void* w, const Unit& u, float (&x)[2 * V]) {
@@ -138,7 +146,9 @@ __device__ __forceinline__ void load_weights(const QkNormArgs& a, const void* w,
 #pragma unroll
     for (int e = 0; e < 2 * V; ++e) x[e] = 1.0f;
   } else if (a.weight_bf16) {
-    load_unit<bf16, V>((const bf16*)w, u, x);
+    RawUnit<bf16, V> r;
+    r.load((const bf16*)w, u);
+    r.values(x);
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -189,130 +199,149 @@ __device__ __forceinline__ int64_t row_at(const Strides& s, int T, int64_t token
   return b * s.b + h * s.h + (token - b * T) * s.t;
 }
 
+// The rows of one tensor and up to tpw tokens from n0 on, kT / LG at a time. The first rows are on their way while the
+// angles are formed, the next while one is worked on.
+template <int LG>
+struct Rows {
+  int64_t n0;
+  int nt, H, rows, grp;
+  __device__ __forceinline__ Rows(const QkNormArgs& a, const NormTensor& s, int64_t first, int tpw)
+      : n0(first), nt((int)min((int64_t)tpw, a.tokens - first)), H(s.H), rows(nt * s.H), grp(threadIdx.x / LG) {}
+  // token and head of row i0 + grp (the last row again behind it: every lane of a wave reaches the reductions)
+  __device__ __forceinline__ int token(int i0) const { return min(i0 + grp, rows - 1) / H; }
+  __device__ __forceinline__ int64_t at(const QkNormArgs& a, const Strides& s, int i0) const {
+    const int i = min(i0 + grp, rows - 1), n = i / H;
+    return row_at(s, a.T, n0 + n, i - n * H);
+  }
+  __device__ __forceinline__ bool mine(int i0) const { return i0 + grp < rows; }
+};
+
 template <typename TI, int V, int LG, bool INTER>
-__global__ __launch_bounds__(kT) void qk_norm_fwd_kernel(QkNormArgs a, int tpw) {
+__global__ __launch_bounds__(kT) void qk_norm_fwd_kernel(QkNormArgs a, int tpw, int first_k) {
   extern __shared__ float2 cs[];  // [tpw][rope_dim / 2]
   __shared__ int live[kMaxTokens];
-  const int64_t n0 = (int64_t)blockIdx.x * tpw;
-  const int nt = (int)min((int64_t)tpw, a.tokens - n0);
-  token_angles(a, n0, nt, cs, live);
-  __syncthreads();
-  const int grp = threadIdx.x / LG;
+  const bool second = (int)blockIdx.x >= first_k;
+  const NormTensor s = a.s[second];
   const Unit u = unit_of<V>(a, threadIdx.x % LG);
   const float inv_d = 1.0f / (float)a.D;
+  const Rows<LG> r(a, s, (int64_t)(blockIdx.x - (second ? first_k : 0)) * tpw, tpw);
+  RawUnit<TI, V> next;
+  next.load((const TI*)s.x + r.at(a, s.sx, 0), u);
+  float w[2 * V];
+  load_weights<V>(a, s.w, u, w);
+  token_angles(a, r.n0, r.nt, cs, live);
+  __syncthreads();
+  for (int i0 = 0; i0 < r.rows; i0 += kT / LG) {
+    float x[2 * V];
+    next.values(x);
+    if (i0 + kT / LG < r.rows) next.load((const TI*)s.x + r.at(a, s.sx, i0 + kT / LG), u);
+    const int n = r.token(i0);
+    if (a.norm) {
+      float q = 0.0f;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const NormTensor& s = a.s[which];
-    if (s.H == 0) continue;
-    float w[2 * V];
-    load_weights<V>(a, s.w, u, w);
-    const int rows = nt * s.H;
-    for (int i0 = 0; i0 < rows; i0 += kT / LG) {  // every lane of a wave reaches the reduction
-      const int i = min(i0 + grp, rows - 1), n = i / s.H, h = i - n * s.H;
-      float x[2 * V];
-      load_unit<TI, V>((const TI*)s.x + row_at(s.sx, a.T, n0 + n, h), u, x);
-      if (a.norm) {
-        float q = 0.0f;
+      for (int e = 0; e < 2 * V; ++e) q = __builtin_fmaf(x[e], x[e], q);
+      const float c = 1.0f / sqrtf(lane_group_sum<LG>(q) * inv_d + a.eps);
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) q = __builtin_fmaf(x[e], x[e], q);
-        const float r = 1.0f / sqrtf(lane_group_sum<LG>(q) * inv_d + a.eps);
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) x[e] = x[e] * r * w[e];
-      }
-      if (u.turned) turn<V, INTER, false>(x, cs + n * (a.rope_dim >> 1) + u.j0);
-      if (!live[n]) {
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) x[e] = 0.0f;
-      }
-      if (i0 + grp < rows) store_unit<TI, V>((TI*)s.y + row_at(s.sy, a.T, n0 + n, h), u, x);
+      for (int e = 0; e < 2 * V; ++e) x[e] = x[e] * c * w[e];
     }
+    if (u.turned) turn<V, INTER, false>(x, cs + n * (a.rope_dim >> 1) + u.j0);
+    if (!live[n]) {
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) x[e] = 0.0f;
+    }
+    if (r.mine(i0)) store_unit<TI, V>((TI*)s.y + r.at(a, s.sy, i0), u, x);
   }
 }
 
-// A workgroup goes over every gridDim.x-th run of tokens and keeps its sums for the weights in registers: a lane has
-// the same channels in every row. At the end the workgroup's groups of lanes meet in LDS in a fixed order.
+// A workgroup goes over every so-many-th run of a tensor's tokens and keeps its sums for the weights in registers: a
+// lane has the same channels in every row. At the end the workgroup's groups of lanes meet in LDS in a fixed order.
 template <typename TI, int V, int LG, bool INTER>
 __global__ __launch_bounds__(kT) void qk_norm_bwd_kernel(QkNormArgs a, int tpw) {
   extern __shared__ float2 cs[];
   __shared__ int live[kMaxTokens];
   __shared__ float sums[kT / LG][2 * V * LG + 1];
+  const bool second = (int)blockIdx.x >= a.groups[0];
+  const int group = blockIdx.x - (second ? a.groups[0] : 0), groups = a.groups[second];
+  const NormTensor s = a.s[second];
   const int grp = threadIdx.x / LG, lane = threadIdx.x % LG;
   const Unit u = unit_of<V>(a, lane);
   const float inv_d = 1.0f / (float)a.D;
-  float dw[2][2 * V];
+  float w[2 * V], dw[2 * V];
+  load_weights<V>(a, s.w, u, w);
 #pragma unroll
-  for (int e = 0; e < 2 * V; ++e) dw[0][e] = dw[1][e] = 0.0f;
-  for (int64_t n0 = (int64_t)blockIdx.x * tpw; n0 < a.tokens; n0 += (int64_t)gridDim.x * tpw) {
-    const int nt = (int)min((int64_t)tpw, a.tokens - n0);
+  for (int e = 0; e < 2 * V; ++e) dw[e] = 0.0f;
+  for (int64_t n0 = (int64_t)group * tpw; n0 < a.tokens; n0 += (int64_t)groups * tpw) {
+    const Rows<LG> r(a, s, n0, tpw);
+    RawUnit<TI, V> xn, gn;
+    xn.load((const TI*)s.x + r.at(a, s.sx, 0), u);
+    gn.load((const TI*)s.dy + r.at(a, s.sdy, 0), u);
     __syncthreads();  // the angles before are read
-    token_angles(a, n0, nt, cs, live);
+    token_angles(a, n0, r.nt, cs, live);
     __syncthreads();
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const NormTensor& s = a.s[which];
-      if (s.H == 0) continue;
-      float w[2 * V];
-      load_weights<V>(a, s.w, u, w);
-      const int rows = nt * s.H;
-      for (int i0 = 0; i0 < rows; i0 += kT / LG) {
-        const int i = min(i0 + grp, rows - 1), n = i / s.H, h = i - n * s.H;
-        const bool mine = i0 + grp < rows;
-        float x[2 * V], g[2 * V];
-        load_unit<TI, V>((const TI*)s.x + row_at(s.sx, a.T, n0 + n, h), u, x);
-        load_unit<TI, V>((const TI*)s.dy + row_at(s.sdy, a.T, n0 + n, h), u, g);
-        if (u.turned) turn<V, INTER, true>(g, cs + n * (a.rope_dim >> 1) + u.j0);
-        if (a.norm) {
-          float q = 0.0f, d = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 2 * V; ++e) {
-            q = __builtin_fmaf(x[e], x[e], q);
-            d = __builtin_fmaf(g[e] * w[e], x[e], d);
-          }
-          const float r = 1.0f / sqrtf(lane_group_sum<LG>(q) * inv_d + a.eps);
-          const float k = lane_group_sum<LG>(d) * r * inv_d;  // mean(g w x r)
-          const bool counts = mine && live[n];
-#pragma unroll
-          for (int e = 0; e < 2 * V; ++e) {
-            const float xr = x[e] * r;
-            if (counts) dw[which][e] = __builtin_fmaf(g[e], xr, dw[which][e]);
-            g[e] = r * (g[e] * w[e] - xr * k);
-          }
-        }
-        if (!live[n]) {
-#pragma unroll
-          for (int e = 0; e < 2 * V; ++e) g[e] = 0.0f;
-        }
-        if (mine) store_unit<TI, V>((TI*)s.y + row_at(s.sy, a.T, n0 + n, h), u, g);
+    for (int i0 = 0; i0 < r.rows; i0 += kT / LG) {
+      float x[2 * V], g[2 * V];
+      xn.values(x);
+      gn.values(g);
+      if (i0 + kT / LG < r.rows) {
+        xn.load((const TI*)s.x + r.at(a, s.sx, i0 + kT / LG), u);
+        gn.load((const TI*)s.dy + r.at(a, s.sdy, i0 + kT / LG), u);
       }
+      const int n = r.token(i0);
+      if (u.turned) turn<V, INTER, true>(g, cs + n * (a.rope_dim >> 1) + u.j0);
+      const bool mine = r.mine(i0);
+      if (a.norm) {
+        float q = 0.0f, d = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          q = __builtin_fmaf(x[e], x[e], q);
+          d = __builtin_fmaf(g[e] * w[e], x[e], d);
+        }
+        const float c = 1.0f / sqrtf(lane_group_sum<LG>(q) * inv_d + a.eps);
+        const float k = lane_group_sum<LG>(d) * c * inv_d;  // mean(g w x c)
+        const bool counts = mine && live[n];
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+          const float xc = x[e] * c;
+          if (counts) dw[e] = __builtin_fmaf(g[e], xc, dw[e]);
+          g[e] = c * (g[e] * w[e] - xc * k);
+        }
+      }
+      if (!live[n]) {
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) g[e] = 0.0f;
+      }
+      if (mine) store_unit<TI, V>((TI*)s.y + r.at(a, s.sy, i0), u, g);
     }
   }
-  for (int which = 0; which < 2; ++which) {
-    if (!a.s[which].dw || a.s[which].H == 0) continue;
-    __syncthreads();
+  if (!s.dw) return;
 #pragma unroll
-    for (int e = 0; e < 2 * V; ++e) sums[grp][e * LG + lane] = dw[which][e];
-    __syncthreads();
-    // thread (e, lane): the sum over the groups, to the channel that it is
-    for (int i = threadIdx.x; i < 2 * V * LG; i += kT) {
-      const int e = i / LG;
-      const Unit v = unit_of<V>(a, i % LG);
-      float s = 0.0f;
-      for (int x = 0; x < kT / LG; ++x) s += sums[x][i];
-      const int ch = e < V ? v.a + e : v.b + e - V;
-      if (e < V ? v.some : v.both) a.ws[((int64_t)which * a.groups + blockIdx.x) * a.D + ch] = s;
-    }
+  for (int e = 0; e < 2 * V; ++e) sums[grp][e * LG + lane] = dw[e];
+  __syncthreads();
+  // thread (e, lane): the sum over the groups, to the channel that it is
+  float* part = a.ws + (second ? (int64_t)a.groups[0] * a.D : 0);  // [D][groups]
+  for (int i = threadIdx.x; i < 2 * V * LG; i += kT) {
+    const int e = i / LG;
+    const Unit v = unit_of<V>(a, i % LG);
+    float t = 0.0f;
+    for (int x = 0; x < kT / LG; ++x) t += sums[x][i];
+    const int ch = e < V ? v.a + e : v.b + e - V;
+    if (e < V ? v.some : v.both) part[(int64_t)ch * groups + group] = t;
   }
 }
 
 // Channel blockIdx.x of either weight: the workgroups' sums, in a fixed order.
-__global__ __launch_bounds__(64) void qk_norm_sum_kernel(QkNormArgs a) {
-  const int ch = blockIdx.x, which = blockIdx.y;
-  if (!a.s[which].dw) return;
+__global__ __launch_bounds__(kT) void qk_norm_sum_kernel(QkNormArgs a) {
+  __shared__ float waves[kT / 64];
+  const int ch = blockIdx.x, second = blockIdx.y, groups = a.groups[second];
+  if (!a.s[second].dw) return;
+  const float* part = a.ws + (second ? (int64_t)a.groups[0] * a.D : 0) + (int64_t)ch * groups;
   float s = 0.0f;
-  if (a.s[which].H)
-    for (int g = threadIdx.x; g < a.groups; g += 64) s += a.ws[((int64_t)which * a.groups + g) * a.D + ch];
+#pragma unroll 4
+  for (int g = threadIdx.x; g < groups; g += kT) s += part[g];
   s = lane_group_sum<64>(s);
-  if (threadIdx.x == 0) a.s[which].dw[ch] = s;
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) a.s[second].dw[ch] = (waves[0] + waves[1]) + (waves[2] + waves[3]);
 }
 
 constexpr int lanes_for(int units) { return units <= 1 ? 1 : units <= 2 ? 2 : units <= 4 ? 4 : units <= 8 ? 8 : units <= 16 ? 16 : units <= 32 ? 32 : 64; }
@@ -324,21 +353,22 @@ int piece_of(const QkNormArgs& a, int widest) {
   return 1;
 }
 
-int tokens_per_group(const QkNormArgs& a) { return a.tokens >= 4096 ? kMaxTokens : 1; }
+int tokens_per_group(int64_t tokens) { return tokens >= 4096 ? kMaxTokens : 1; }
 
 struct Forward {
   template <typename TI, int V, int LG, bool INTER>
   static void go(const QkNormArgs& a, hipStream_t stream) {
-    const int tpw = tokens_per_group(a);
-    hipLaunchKernelGGL((qk_norm_fwd_kernel<TI, V, LG, INTER>), dim3((unsigned)((a.tokens + tpw - 1) / tpw)), dim3(kT),
-                       (size_t)tpw * (a.rope_dim / 2) * sizeof(float2), stream, a, tpw);
+    const int tpw = tokens_per_group(a.tokens);
+    const int64_t runs = (a.tokens + tpw - 1) / tpw, q = a.s[0].H ? runs : 0, k = a.s[1].H ? runs : 0;
+    hipLaunchKernelGGL((qk_norm_fwd_kernel<TI, V, LG, INTER>), dim3((unsigned)(q + k)), dim3(kT),
+                       (size_t)tpw * (a.rope_dim / 2) * sizeof(float2), stream, a, tpw, (int)q);
   }
 };
 struct Backward {
   template <typename TI, int V, int LG, bool INTER>
   static void go(const QkNormArgs& a, hipStream_t stream) {
-    const int tpw = tokens_per_group(a);
-    hipLaunchKernelGGL((qk_norm_bwd_kernel<TI, V, LG, INTER>), dim3((unsigned)a.groups), dim3(kT),
+    const int tpw = tokens_per_group(a.tokens);
+    hipLaunchKernelGGL((qk_norm_bwd_kernel<TI, V, LG, INTER>), dim3((unsigned)(a.groups[0] + a.groups[1])), dim3(kT),
                        (size_t)tpw * (a.rope_dim / 2) * sizeof(float2), stream, a, tpw);
   }
 };
@@ -381,9 +411,7 @@ hipError_t dispatch(const QkNormArgs& a, int dtype, hipStream_t stream) {
 }  // namespace
 
 int qk_norm_groups(int64_t tokens) {
-  QkNormArgs a{};
-  a.tokens = tokens;
-  const int tpw = tokens_per_group(a);
+  const int tpw = tokens_per_group(tokens);
   const int64_t n = (tokens + tpw - 1) / tpw;
   return (int)(n < kMaxGroups ? n : kMaxGroups);
 }
@@ -392,12 +420,17 @@ hipError_t launch_qk_norm_fwd(const QkNormArgs& a, int dtype, hipStream_t stream
   return dispatch<Forward>(a, dtype, stream);
 }
 
-hipError_t launch_qk_norm_bwd(const QkNormArgs& a, int dtype, hipStream_t stream) {
-  if (a.groups) {
+hipError_t launch_qk_norm_bwd(const QkNormArgs& given, int dtype, hipStream_t stream) {
+  QkNormArgs a = given;
+  const int most = qk_norm_groups(a.tokens);
+  for (int i = 0; i < 2; ++i) a.groups[i] = a.s[i].H ? most : 0;
+  if (a.tokens && a.groups[0] + a.groups[1]) {
     const hipError_t e = dispatch<Backward>(a, dtype, stream);
     if (e != hipSuccess) return e;
+  } else {
+    a.groups[0] = a.groups[1] = 0;
   }
-  if (a.s[0].dw || a.s[1].dw) hipLaunchKernelGGL(qk_norm_sum_kernel, dim3((unsigned)a.D, 2), dim3(64), 0, stream, a);
+  if (a.s[0].dw || a.s[1].dw) hipLaunchKernelGGL(qk_norm_sum_kernel, dim3((unsigned)a.D, 2), dim3(kT), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -221,7 +221,7 @@ rel_status relation_qk_norm_bwd(const rel_qk_norm* p, const void* q, const void*
   a.s[0] = {q, q_weight, dq_out, dq, strides_of(p->q), strides_of(p->q_out), strides_of(p->dq), dq_weight, has[0] ? (int)p->Hq : 0};
   a.s[1] = {k, k_weight, dk_out, dk, strides_of(p->k), strides_of(p->k_out), strides_of(p->dk), dk_weight, has[1] ? (int)p->H : 0};
   a.ws = (float*)workspace;
-  a.groups = empty ? 0 : rel::qk_norm_groups(a.tokens);
+  if (empty) a.tokens = 0;
   return hip_status(rel::launch_qk_norm_bwd(a, p->dtype, (hipStream_t)stream), "qk norm backward launch");
 }
 

@@ -31,11 +31,11 @@ struct QkNormArgs {
   int T, D;
   int rope_dim, interleaved, norm, weight_bf16;
   float eps, amplitude;
-  float* ws;                 // backward: partial sums of the weights' gradients, [2][groups][D]
-  int groups;
+  float* ws;                 // backward: partial sums of the weights' gradients, [D][groups] of either tensor
+  int groups[2];             // workgroups of either tensor (set by the launch)
   double turns[64];          // turns of channel pair j per position
 };
-// Workgroups of the backward pass, each with a row of partial sums.
+// The most workgroups that the backward pass has of one tensor, each with a partial sum of every channel.
 int qk_norm_groups(int64_t tokens);
 hipError_t launch_qk_norm_fwd(const QkNormArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_qk_norm_bwd(const QkNormArgs& a, int dtype, hipStream_t stream);
