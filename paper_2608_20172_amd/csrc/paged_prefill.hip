@@ -31,7 +31,8 @@ namespace {
 
 constexpr int kNT = 256;   // threads of a workgroup
 constexpr int kBK = 64;    // keys of a tile
-constexpr int kRows = 128; // rows of a tile
+constexpr int kRows = 128; // rows of a tile, 32 a wave
+constexpr int kFewRows = 32;  // rows of a tile that the four waves share
 constexpr unsigned kMany = 1u << 30;
 constexpr int kNone = 0x7fffffff;
 
@@ -44,7 +45,7 @@ __device__ __forceinline__ int tokens_of(const PagedPrefillArgs& a, int b, int& 
 }
 __device__ __forceinline__ int tiles_of(const PagedPrefillArgs& a, int b) {
   int first;
-  return (tokens_of(a, b, first) * a.G + kRows - 1) / kRows;
+  return (tokens_of(a, b, first) * a.G + a.tile_rows - 1) / a.tile_rows;
 }
 
 // Request and tile of it that tile t of the batch is; false past the last. All threads call it; place has two ints.
@@ -221,12 +222,119 @@ __device__ __forceinline__ void slow_keys64(const unsigned char* Ks, const unsig
   }
 }
 
-// A row of a tile: its index in q and out, and its position.
+// A tile of a step: rows row0 .. row0 + rows - 1 of request b at key head h, over the key tiles kt0 .. nkt - 1.
+struct Tile {
+  int b, h, first, n, len;  // the request's first token and their number, its length
+  int row0, rows;
+  int slice, kt0, nkt;
+  bool few;                 // the four waves share the rows
+};
+// A row of it: its index in q and out, and its position.
 struct TileRow {
   bool live;
   int64_t at;  // row of q, out and row_stat
   int pos;     // from 0; -1: no row
 };
+__device__ __forceinline__ TileRow row_of(const PagedPrefillArgs& a, const Tile& t, int r) {
+  const int x = t.row0 + min(r, t.rows - 1), tok = x / a.G;
+  TileRow y;
+  y.live = r < t.rows;
+  y.at = (int64_t)(t.first + tok) * a.Hq + t.h * a.G + (x - tok * a.G);
+  y.pos = y.live ? t.len - t.n + tok : -1;
+  return y;
+}
+__device__ __forceinline__ int position_of(const PagedPrefillArgs& a, const Tile& t, int r) {
+  return t.len - t.n + (t.row0 + min(r, t.rows - 1)) / a.G;
+}
+template <typename E>
+__device__ __forceinline__ const char* head_of(const PagedPrefillArgs& a, const void* pool, int h) {
+  return (const char*)pool + (int64_t)h * a.c.sh * (int64_t)sizeof(E);
+}
+
+// The row of this lane (and of the one 32 away) from its terminal state: into out, or into the slice's states.
+template <class P, int D>
+__device__ __forceinline__ void finish_tile_row(const PagedPrefillArgs& a, const Tile& t, const TileRow& me, float m, float l,
+                                                float uii, const floatx16 (&oacc)[D / 32], int bad_key, const Lane& L) {
+  using E = typename P::T;
+  constexpr int DB = D / 32;
+  const int width = a.c.D;
+  const float total = l + xor32(l);
+  const float un = (uii + xor32(uii)) * (sizeof(E) == 4 ? 1.0f : a.scale * kLog2e);  // one of the two has it, the other 0
+  if (!me.live) return;
+  const bool lost = bad_key <= me.pos || total != total;  // a page outside the pool, or a NaN among the keys
+  if (a.nsplit > 1) {
+    float* st = a.states + ((int64_t)t.slice * a.N * a.Hq + me.at) * (width + 2);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int d0 = 32 * db + 8 * rq + 4 * L.g;
+        if (d0 >= width) continue;
+#pragma unroll
+        for (int e = 0; e < 4; e += 2)  // 8-byte aligned: the width is a multiple of 4
+          *reinterpret_cast<float2*>(st + 2 + d0 + e) = float2{oacc[db][4 * rq + e], oacc[db][4 * rq + e + 1]};
+      }
+    }
+    if (L.g == 0) *reinterpret_cast<float2*>(st) = float2{m, lost ? __builtin_nanf("") : total};
+    return;
+  }
+  const float lam = *a.lambda;
+  const float ln_i = logf((float)(me.pos + 1));
+  const RowEpilogue e = row_epilogue(m, total, un, a.inv_tau, lam, ln_i);
+  int64_t off;
+  entry_offset(a, t.b, t.h, me.pos, off);
+  const E* vi = (const E*)a.v + off;
+  E* o = (E*)a.out + me.at * width;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const int d0 = 32 * db + 8 * rq + 4 * L.g;
+      if (d0 >= width) continue;
+      const floatx4 x = P::load4(vi + d0);
+      floatx4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        y[i] = lost ? __builtin_nanf("") : __builtin_fmaf(e.omg, x[i], e.inv_l * oacc[db][4 * rq + i]);
+      P::store4(o + d0, y);
+    }
+  }
+  if (L.g == 0 && a.row_stat) a.row_stat[me.at] = lost ? __builtin_nanf("") : e.lnZ + lam * ln_i;
+}
+
+// The scan of a tile again, by the waves whose first one failed its check (redo); all of them load. A function of its
+// own, so that its registers are not the fast scan's.
+template <class P, int D>
+__device__ __attribute__((noinline)) void scan_again(PagedPrefillArgs a, Tile t, bool redo, int bad_key, unsigned char* K0,
+                                                     unsigned char* V0, unsigned char* K1, unsigned char* V1) {
+  using E = typename P::T;
+  constexpr int QM = sizeof(E) == 4 ? 1 : 0;
+  constexpr int KS = D / 16, DB = D / 32;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const Lane L(lane);
+  const int wrow = t.few ? 0 : 32 * w, jlast = position_of(a, t, t.rows - 1);
+  const TileRow me = row_of(a, t, wrow + L.n);
+  const int plo = position_of(a, t, wrow), phi = wrow < t.rows ? position_of(a, t, wrow + 31) : -1;
+  const float c = a.scale * kLog2e;
+  const char *k = head_of<E>(a, a.k, t.h), *v = head_of<E>(a, a.v, t.h);
+  const int32_t* trow = a.table + (int64_t)t.b * a.W;
+  typename P::Op qop[KS];
+  load_row<P, KS, QM>((const E*)a.q + me.at * a.c.D, me.live, a.c.D, L, c, qop);
+  float m = 0.0f, l = 0.0f, uii = 0.0f;
+  floatx16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = floatx16{};
+  int bad = kNone, id[Gather<P>::ROWS];
+  for (int kt = t.kt0; kt < t.nkt; ++kt) {
+    const bool odd = kt & 1;
+    look_up<P>(a, trow, kt, w, lane, jlast, id);
+    load_tile<P>(a, k, v, kt, w, lane, jlast, id, odd ? K1 : K0, odd ? V1 : V0, bad);
+    wait_loads();
+    __syncthreads();  // the other buffer is read up to here
+    if (redo) slow_keys64<P, D, QM>(odd ? K1 : K0, odd ? V1 : V0, kt * kBK, plo, phi, me.pos, qop, oacc, m, l, uii, L, lane, c);
+  }
+  if (redo) finish_tile_row<P, D>(a, t, me, m, l, uii, oacc, bad_key, L);
+}
 
 template <class P, int D>
 constexpr int prefill_occupancy() {
@@ -246,45 +354,44 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
   __shared__ __attribute__((aligned(1024))) unsigned char KB[TB];
   __shared__ __attribute__((aligned(1024))) unsigned char VB[TB];
   __shared__ int place[2], bad_key;
+  __shared__ float shared_l[kNT / 64][64], shared_u[kNT / 64][64];
   __shared__ unsigned wsum[kNT / 64];
 
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const Lane L(lane);
-  int h, tile, b, own;
-  if (!map_tile(a.map, blockIdx.x, h, tile, true)) return;
+  Tile t;
+  int item, own;
+  if (!map_tile(a.map, blockIdx.x, t.h, item, true)) return;
+  t.slice = item / a.tiles;
   if (tid == 0) bad_key = kNone;
-  if (!find_tile(a, (unsigned)tile, b, own, place, wsum)) return;
-  int first;
-  const int n = tokens_of(a, b, first), len = a.lengths[b];
+  if (!find_tile(a, (unsigned)(item - t.slice * a.tiles), t.b, own, place, wsum)) return;
+  t.n = tokens_of(a, t.b, t.first);
+  t.len = a.lengths[t.b];
+  t.row0 = own * a.tile_rows;
+  t.rows = min(a.tile_rows, t.n * a.G - t.row0);
+  t.few = t.rows <= kFewRows;
   const int width = a.c.D;
-  const int row0 = own * kRows, rows = min(kRows, n * a.G - row0);
-  auto row_of = [&](int r) __attribute__((always_inline)) {
-    const int x = row0 + min(r, rows - 1), tok = x / a.G;
-    TileRow t;
-    t.live = r < rows;
-    t.at = (int64_t)(first + tok) * a.Hq + h * a.G + (x - tok * a.G);
-    t.pos = t.live ? len - n + tok : -1;
-    return t;
-  };
-  if (len < n || len > a.max_len) {  // the error is seen
-    for (int x = tid; x < rows * width; x += kNT) {
+  if (t.len < t.n || t.len > a.max_len) {  // the error is seen (with several slices the merge sees it)
+    if (a.nsplit > 1) return;
+    for (int x = tid; x < t.rows * width; x += kNT) {
       const int r = x / width;
-      Elem<E>::store((E*)a.out + row_of(r).at * width + (x - r * width), __builtin_nanf(""));
+      Elem<E>::store((E*)a.out + row_of(a, t, r).at * width + (x - r * width), __builtin_nanf(""));
     }
-    if (a.row_stat && tid < rows) a.row_stat[row_of(tid).at] = __builtin_nanf("");
+    if (a.row_stat && tid < t.rows) a.row_stat[row_of(a, t, tid).at] = __builtin_nanf("");
     return;
   }
-  const int p0 = len - n;
-  const int wrow = 32 * w;
-  const TileRow me = row_of(wrow + L.n);
-  // positions: of the tile's first and last row, and of this wave's
-  const int tlo = p0 + row0 / a.G, jlast = p0 + (row0 + rows - 1) / a.G;
-  const int plo = p0 + (row0 + min(wrow, rows - 1)) / a.G;
-  const int phi = wrow < rows ? p0 + (row0 + min(wrow + 31, rows - 1)) / a.G : -1;
+  const int jlast = position_of(a, t, t.rows - 1);  // the last row's position
+  t.kt0 = t.slice * (a.slice / kBK);
+  t.nkt = min(t.kt0 + a.slice / kBK, jlast / kBK + 1);
+  const int kt0 = t.kt0, nkt = t.nkt;
+  if (kt0 >= nkt) return;  // a slice behind every row: nobody reads its states
+  const bool few = t.few;  // the four waves share the rows and take a block of 32 keys each
+  const int wrow = few ? 0 : 32 * w;
+  TileRow me = row_of(a, t, wrow + L.n);
+  const int tlo = position_of(a, t, 0);  // the first row's position
   const float c = a.scale * kLog2e;
-  const char* k = (const char*)a.k + (int64_t)h * a.c.sh * (int64_t)sizeof(E);
-  const char* v = (const char*)a.v + (int64_t)h * a.c.sh * (int64_t)sizeof(E);
-  const int32_t* trow = a.table + (int64_t)b * a.W;
+  const char *k = head_of<E>(a, a.k, t.h), *v = head_of<E>(a, a.v, t.h);
+  const int32_t* trow = a.table + (int64_t)t.b * a.W;
 
   if (width < D) {  // channels past the cache's width: zeros that no load overwrites
     for (int x = tid; x < TB / 16; x += kNT) {
@@ -304,104 +411,168 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = floatx16{};
   int bad = kNone;
-  const int nkt = jlast / kBK + 1;
   int id[Gather<P>::ROWS];
   auto load = [&](int kt, unsigned char* Kd, unsigned char* Vd) __attribute__((always_inline)) {
     load_tile<P>(a, k, v, kt, w, lane, jlast, id, Kd, Vd, bad);
     look_up<P>(a, trow, kt + 1, w, lane, jlast, id);  // past the last tile: the last key's page again
   };
-  auto fast_step = [&](auto full, int kt, const unsigned char* Ks, const unsigned char* Vs, unsigned char* Kn,
-                       unsigned char* Vn) __attribute__((always_inline)) {
-    wait_loads();      // this wave's part of tile kt is in LDS, and the page ids of tile kt + 1 are here
-    __syncthreads();   // ... and every wave's; tile kt - 1 is no longer read
-    if (kt + 1 < nkt) load(kt + 1, Kn, Vn);
-    if (decltype(full)::value)
-      full_keys64<P, D, QM>(Ks, Vs, 0, qop, oacc, m, l, uii, L, c);
-    else
-      masked_keys64<P, D, QM>(Ks, Vs, kt * kBK, phi, me.pos, qop, oacc, m, l, uii, L, c);
-  };
-  auto run_fast = [&](int ka, int kb, auto full) __attribute__((always_inline)) {
-    int kt = ka;
-    if (kt < kb && (kt & 1)) {
-      fast_step(full, kt, KB, VB, KA, VA);
-      ++kt;
+  look_up<P>(a, trow, kt0, w, lane, jlast, id);
+  if (few) {
+    // 128 keys at a time: waves 0, 1 the blocks of the first tile, waves 2, 3 those of the second
+    for (int kt = kt0; kt < nkt; kt += 2) {
+      if (kt > kt0) __syncthreads();  // the tiles before are read
+      load(kt, KA, VA);
+      load(kt + 1, KB, VB);
+      wait_loads();
+      __syncthreads();
+      const int k0 = (kt + (w >> 1)) * kBK + 32 * (w & 1), krow = 32 * (w & 1);
+      const unsigned char* Ks = w >> 1 ? KB : KA;
+      const unsigned char* Vs = w >> 1 ? VB : VA;
+      Op pop[2] = {Op{}, Op{}};
+      if (k0 <= jlast) {
+        const floatx16 s = evidence<P, KS>(Ks, krow, qop, L);
+        fast_block<P, D, QM, true>(s, m, l, uii, pop, L, me.pos - k0, c);
+      }
+      add_values<P, D>(Vs, krow, 0, pop, oacc, L);
     }
-    for (; kt < kb; kt += 2) {
-      fast_step(full, kt, KA, VA, KB, VB);
-      if (kt + 1 < kb) fast_step(full, kt + 1, KB, VB, KA, VA);
-    }
-  };
-  look_up<P>(a, trow, 0, w, lane, jlast, id);
-  load(0, KA, VA);
-  const int kf = min(tlo / kBK, nkt);  // tiles before every row's position
-  run_fast(0, kf, std::true_type{});
-  run_fast(kf, nkt, std::false_type{});
+  } else {
+    const int phi = wrow < t.rows ? position_of(a, t, wrow + 31) : -1;  // the wave's last position
+    auto fast_step = [&](auto full, int kt, const unsigned char* Ks, const unsigned char* Vs, unsigned char* Kn,
+                         unsigned char* Vn) __attribute__((always_inline)) {
+      wait_loads();      // this wave's part of tile kt is in LDS, and the page ids of tile kt + 1 are here
+      __syncthreads();   // ... and every wave's; tile kt - 1 is no longer read
+      if (kt + 1 < nkt) load(kt + 1, Kn, Vn);
+      if (decltype(full)::value)
+        full_keys64<P, D, QM>(Ks, Vs, 0, qop, oacc, m, l, uii, L, c);
+      else
+        masked_keys64<P, D, QM>(Ks, Vs, kt * kBK, phi, me.pos, qop, oacc, m, l, uii, L, c);
+    };
+    auto run_fast = [&](int ka, int kb, auto full) __attribute__((always_inline)) {
+      int kt = ka;
+      if (kt < kb && (kt & 1)) {
+        fast_step(full, kt, KB, VB, KA, VA);
+        ++kt;
+      }
+      for (; kt < kb; kt += 2) {
+        fast_step(full, kt, KA, VA, KB, VB);
+        if (kt + 1 < kb) fast_step(full, kt + 1, KB, VB, KA, VA);
+      }
+    };
+    load(kt0, KA, VA);                                  // kt0 is even
+    const int kf = max(kt0, min(tlo / kBK, nkt));       // tiles before every row's position
+    run_fast(kt0, kf, std::true_type{});
+    run_fast(kf, nkt, std::false_type{});
+  }
   if (bad != kNone) atomicMin(&bad_key, bad);
   // As in the fused forward pass the scan ran with the reference at 0, which is exact while the row total stays under
-  // 2^64. Sums that are not finite come from values that are not, perhaps behind the row.
+  // 2^64 (2^62 in each of four waves). Sums that are not finite come from values that are not, perhaps behind the row.
   const float lt = l + xor32(l);
   float f = 0.0f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) f = __builtin_fmaf(oacc[db][r], 0.0f, f);
-  const bool again = me.live && (!(lt <= kSpecMax) || f != f);
-  if (__syncthreads_or(again ? 1 : 0)) {
-    const bool redo = wave_any(again);
-    if (redo) {
-      m = l = uii = 0.0f;
+  const bool again = me.live && (!(lt <= kSpecMax * 0.25f) || f != f);
+  const bool any = __syncthreads_or(again ? 1 : 0);
+  if (few && !any) {
+    // the waves' sums meet in the tiles' memory, which the barrier has freed, and the first wave has them all
+    if (w > 0) {
+      float* z = reinterpret_cast<float*>(w == 1 ? VA : w == 2 ? KB : VB);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) oacc[db] = floatx16{};
+      for (int x = 0; x < 4 * DB; ++x)
+        *reinterpret_cast<floatx4*>(z + (x * 64 + lane) * 4) =
+            floatx4{oacc[x / 4][4 * (x % 4)], oacc[x / 4][4 * (x % 4) + 1], oacc[x / 4][4 * (x % 4) + 2],
+                    oacc[x / 4][4 * (x % 4) + 3]};
+      shared_l[w][lane] = l;
+      shared_u[w][lane] = uii;
     }
-    look_up<P>(a, trow, 0, w, lane, jlast, id);
-    load(0, KA, VA);
-    for (int kt = 0; kt < nkt; ++kt) {
-      const bool odd = kt & 1;
-      wait_loads();
-      __syncthreads();
-      if (kt + 1 < nkt) load(kt + 1, odd ? KA : KB, odd ? VA : VB);
-      if (redo)
-        slow_keys64<P, D, QM>(odd ? KB : KA, odd ? VB : VA, kt * kBK, plo, phi, me.pos, qop, oacc, m, l, uii, L, lane, c);
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int x = 0; x < 4 * DB; ++x) {
+      const int at = (x * 64 + lane) * 16;
+      const floatx4 z = (*reinterpret_cast<const floatx4*>(VA + at) + *reinterpret_cast<const floatx4*>(KB + at)) +
+                        *reinterpret_cast<const floatx4*>(VB + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) oacc[x / 4][4 * (x % 4) + i] += z[i];
     }
+    l += (shared_l[1][lane] + shared_l[2][lane]) + shared_l[3][lane];
+    uii += (shared_u[1][lane] + shared_u[2][lane]) + shared_u[3][lane];  // one wave has met the row's own key, the rest 0
   }
-  const float total = l + xor32(l);
-  const float un = (uii + xor32(uii)) * (QM == 0 ? c : 1.0f);  // one lane of the two has it, the other 0
-  if (!me.live) return;
-  const float lam = *a.lambda;
-  const float ln_i = logf((float)(me.pos + 1));
-  const RowEpilogue e = row_epilogue(m, total, un, a.inv_tau, lam, ln_i);
-  const bool lost = bad_key <= me.pos || total != total;  // a page outside the pool, or a NaN among the keys
-  int64_t off;
-  entry_offset(a, b, h, me.pos, off);
-  const E* vi = (const E*)a.v + off;
-  E* o = (E*)a.out + me.at * width;
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-#pragma unroll
-    for (int rq = 0; rq < 4; ++rq) {
-      const int d0 = 32 * db + 8 * rq + 4 * L.g;
-      if (d0 >= width) continue;
-      const floatx4 x = P::load4(vi + d0);
-      floatx4 y;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        y[t] = lost ? __builtin_nanf("") : __builtin_fmaf(e.omg, x[t], e.inv_l * oacc[db][4 * rq + t]);
-      P::store4(o + d0, y);
-    }
+  const bool redo = any && (few ? w == 0 : wave_any(again));
+  if (!redo && !(any && few)) finish_tile_row<P, D>(a, t, me, m, l, uii, oacc, bad_key, L);
+  if (any) scan_again<P, D>(a, t, redo, bad_key, KA, VA, KB, VB);
+}
+
+// The slices of each row joined, with its Self entry, by one wave: lane holds channels lane and lane + 64.
+template <typename TI>
+__global__ __launch_bounds__(kNT) void prefill_merge_kernel(PagedPrefillArgs a) {
+  constexpr int kBatch = 4;
+  const int64_t rows = (int64_t)a.N * a.Hq, at = (int64_t)blockIdx.x * (kNT / 64) + (threadIdx.x >> 6);
+  if (at >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const int tok = (int)(at / a.Hq), hq = (int)(at - (int64_t)tok * a.Hq);
+  int b = 0;  // requests that end before the token
+  for (int x = 0; x < a.B; x += 64) {
+    const bool ends = x + lane < a.B && a.row_start[x + lane + 1] <= tok;
+    b += (int)__popcll(__ballot(ends));
   }
-  if (L.g == 0 && a.row_stat) a.row_stat[me.at] = lost ? __builtin_nanf("") : e.lnZ + lam * ln_i;
+  if (b >= a.B) return;
+  int first;
+  const int n = tokens_of(a, b, first), len = a.lengths[b];
+  if (tok < first || tok >= first + n) return;  // a token of no request
+  const int pos = len >= n && len <= a.max_len ? len - n + tok - first : -1;
+  const SelfEntry self = read_self<TI>(a, b, at, hq, pos + 1, lane);
+  const int D = a.c.D, ns = pos > 0 ? (pos - 1) / a.slice + 1 : 0;  // slices with an Exchange key
+  const int c0 = lane < D ? lane : 0, c1 = lane + 64 < D ? lane + 64 : 0;
+  float m = 0.0f, l = 0.0f, z[2] = {0.0f, 0.0f};
+  for (int s0 = 0; s0 < ns; s0 += kBatch) {
+    float2 ml[kBatch];
+    float zo[kBatch][2];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {  // past the end: the last state again, which counts for nothing
+      const float* st = a.states + ((int64_t)min(s0 + u, ns - 1) * rows + at) * (D + 2);
+      ml[u] = *reinterpret_cast<const float2*>(st);
+      zo[u][0] = st[2 + c0];
+      zo[u][1] = st[2 + c1];
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (s0 + u < ns) merge_into<2>(m, l, z, ml[u].x, ml[u].y, zo[u]);
+  }
+  finish_row<TI>(a, at, pos + 1, lane, self, m, l, z[0], z[1]);
 }
 
 template <class P, int D>
 hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
-  // at most so many tiles: each request has one that is not whole
-  const int64_t tiles = (int64_t)a.N * a.G / kRows + a.B;
-  a.map = make_tilemap(a.c.H, (int)tiles);
+  a.tiles = (int)((int64_t)a.N * a.G / a.tile_rows + a.B);  // each request has one that is not whole
+  a.map = make_tilemap(a.c.H, a.tiles * a.nsplit);
   hipLaunchKernelGGL((prefill_kernel<P, D>), dim3((unsigned)grid_size(a.map)), dim3(kNT), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  const int64_t rows = (int64_t)a.N * a.Hq;
+  hipLaunchKernelGGL((prefill_merge_kernel<typename P::T>), dim3((unsigned)((rows + kNT / 64 - 1) / (kNT / 64))), dim3(kNT), 0,
+                     stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+PrefillPlan paged_prefill_plan(int64_t N, int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype) {
+  constexpr int64_t kTarget = 1024, kMinSlice = 512;
+  PrefillPlan p;
+  auto groups = [&](int64_t rows) { return (N * G / rows + B) * H; };
+  p.tile_rows = groups(kRows) <= 256 && max_len <= 2048 ? kFewRows : kRows;
+  int64_t split = (kTarget + groups(p.tile_rows) - 1) / groups(p.tile_rows);
+  const int64_t most = (max_len + kMinSlice - 1) / kMinSlice;
+  if (split > most) split = most;
+  /*TUNE*/
+  int64_t slice = (max_len + split - 1) / split;
+  slice = (slice + 2 * kBK - 1) / (2 * kBK) * (2 * kBK);  // pairs of tiles
+  p.slice = (int)slice;
+  p.nsplit = (int)((max_len + slice - 1) / slice);
+  return p;
+}
 
 hipError_t launch_paged_prefill(const PagedPrefillArgs& a, int dtype, hipStream_t stream) {
   const int D = a.c.D;

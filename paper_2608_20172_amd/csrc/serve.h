@@ -89,10 +89,19 @@ struct PagedPrefillArgs {
   float scale, inv_tau;
   void* out;                 // [N, Hq, D] dense
   float* row_stat;           // [N, Hq] or null
-  TileMap map;               // key heads x tiles (set by the launch)
+  float* states;             // [nsplit][N Hq][D + 2] (nsplit > 1)
+  int tile_rows;             // rows of a tile
+  int nsplit, slice;         // slices of `slice` keys
+  int tiles;                 // at most so many tiles (set by the launch)
+  TileMap map;               // key heads x tiles x slices (set by the launch)
 };
 // The largest batch: every workgroup finds its tile by a scan over the requests.
 constexpr int kPrefillMaxB = 4096;
+struct PrefillPlan {
+  int tile_rows, nsplit, slice;
+};
+// How a step is cut, by the host's bounds alone.
+PrefillPlan paged_prefill_plan(int64_t N, int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype);
 hipError_t launch_paged_prefill(const PagedPrefillArgs& a, int dtype, hipStream_t stream);
 
 struct SampleArgs {

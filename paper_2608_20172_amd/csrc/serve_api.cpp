@@ -287,7 +287,8 @@ size_t relation_paged_prefill_workspace_bytes(const rel_pages* c, const rel_page
   bool empty = false;
   rel_paged_query q;
   if (check_chunk(c, d, &q, &empty) != REL_OK || empty) return 0;
-  return 0;
+  const rel::PrefillPlan p = rel::paged_prefill_plan(d->N, d->B, c->H, d->Hq / c->H, longest(c, &q), (int)c->D, c->dtype);
+  return p.nsplit == 1 ? 0 : (size_t)p.nsplit * (size_t)(d->N * d->Hq) * (size_t)(c->D + 2) * 4;
 }
 
 rel_status relation_paged_prefill(const rel_pages* c, const rel_paged_chunk* d, const void* q, const void* k_cache,
@@ -332,6 +333,9 @@ rel_status relation_paged_prefill(const rel_pages* c, const rel_paged_chunk* d, 
   a.max_len = (int)longest(c, &as_query);
   a.scale = d->scale > 0.0f ? d->scale : 1.0f / std::sqrt((float)c->D);
   a.inv_tau = 1.0f / d->tau_s;
+  const rel::PrefillPlan plan = rel::paged_prefill_plan(d->N, d->B, c->H, a.G, a.max_len, (int)c->D, c->dtype);
+  a.tile_rows = plan.tile_rows; a.nsplit = plan.nsplit; a.slice = plan.slice;
+  a.states = (float*)workspace;
   a.out = out; a.row_stat = row_stat;
   return hip_status(rel::launch_paged_prefill(a, c->dtype, (hipStream_t)stream), "paged prefill launch");
 }
