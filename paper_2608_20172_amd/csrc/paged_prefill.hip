@@ -5,10 +5,17 @@
 //
 // The scan is that of the fused forward pass (scan.h): 32x32 blocks of transposed
 // evidence, the running reference held at 0 and checked at the end. What differs:
-// * A tile has 128 rows of one request and key head, a row being a (token, query
-//   head) pair with the G query heads of a token side by side, so that a key head
-//   that they share is read once for all. A lane's row has a position of its own,
-//   anywhere in its 32-key block.
+// * A tile has 128 rows of one request and key head, 32 a wave, a row being a
+//   (token, query head) pair with the G query heads of a token side by side, so
+//   that a key head that they share is read once for all. A lane's row has a
+//   position of its own, anywhere in its 32-key block.
+// * A tile of at most 32 rows (a decoding request among chunks, a short chunk) gives
+//   each wave 32 of every 128 keys instead; the four partial sums meet in LDS. With
+//   the reference at 0 they only add. (40 requests that decode and 8 chunks of 128 to
+//   256 tokens over 410 to 4096 keys, 16 heads of width 128 on 4: 194 us with such a
+//   tile's rows all on one wave, now 117.)
+// * Where the tiles leave CUs idle the histories are split into slices whose terminal
+//   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
 //   workgroup finds its tile by a scan over the requests' tile counts in LDS.
 // * A tile of 64 keys is gathered: each lane looks up the page of the key row that
@@ -18,7 +25,15 @@
 // * What stands behind a row in the cache, NaN and infinities included, must not
 //   reach it, but a masked weight of 0 times such a value would: a wave whose sums
 //   are not finite scans again with those values taken apart.
+//
+// What bounds it is the vector work of a weight, about 9 instructions a lane and
+// entry beside one matrix instruction, as in the fused forward pass, and the waits
+// of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
+// 704 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 78 us. On
+// the same rows in one dense tensor the fused forward pass, which looks nothing up,
+// takes 62 us against 73 (8 x 12 x 1536 x 64) and 163 against 199 (4 x 8 x 4096 x 128).
 #include "kernels.h"
+#include "lanes.h"
 #include "paged_row.h"
 #include "scan.h"
 #include "serve.h"
@@ -38,6 +53,14 @@ constexpr int kNone = 0x7fffffff;
 
 __device__ __forceinline__ unsigned add_many(unsigned x, unsigned y) { return min(x + y, kMany); }
 
+// Sum over the wave, of numbers whose sum stays under 2^31 for ascending row starts; others wrap, to some place.
+__device__ __forceinline__ int wave_total(int x) {
+  unsigned u = (unsigned)x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) u += __shfl_xor(u, o, 64);
+  return __builtin_amdgcn_readfirstlane((int)(u & 0x7fffffffu));
+}
+
 // Tokens of request b and the first of them, whatever row_start holds.
 __device__ __forceinline__ int tokens_of(const PagedPrefillArgs& a, int b, int& first) {
   first = min(max(a.row_start[b], 0), a.N);
@@ -48,9 +71,45 @@ __device__ __forceinline__ int tiles_of(const PagedPrefillArgs& a, int b) {
   return (tokens_of(a, b, first) * a.G + a.tile_rows - 1) / a.tile_rows;
 }
 
-// Request and tile of it that tile t of the batch is; false past the last. All threads call it; place has two ints.
-__device__ __forceinline__ bool find_tile(const PagedPrefillArgs& a, unsigned t, int& b, int& own, int* place,
-                                          unsigned* wsum) {
+// Request and tile of it that place t of the batch is; false past the last. A request's last tile, which has the most
+// keys, comes first. Up to 64 requests stand in the lanes of every wave alike. Where they are mostly new (a.level_bits),
+// the last tiles of all requests come first, then the last but one of all, and so on, so that the longest start first:
+// with S(L) the sum of min(tiles, L), t is on level L with S(L) <= t < S(L + 1) (8 prompts of 1024 to 2048 tokens, 12
+// heads x 64: 98 -> 92 us). Else one request after another, whose tiles then share its keys in the L2 (8 chunks of 512
+// after 4096 to 8192 tokens, 32 heads x 128: 514 us, by levels 570).
+__device__ __forceinline__ bool find_tile_64(const PagedPrefillArgs& a, int t, int& b, int& own) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < a.B ? tiles_of(a, lane) : 0;
+  if (!a.level_bits) {
+    unsigned incl = (unsigned)mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned y = __shfl_up(incl, o, 64);
+      if (lane >= o) incl = add_many(incl, y);
+    }
+    const unsigned before = incl - (unsigned)mine;
+    const unsigned long long it = __ballot((unsigned)t >= before && (unsigned)t < incl && mine > 0);
+    if (!it) return false;
+    b = (int)__ffsll((long long)it) - 1;
+    own = __builtin_amdgcn_readfirstlane(__shfl(mine - 1 - (int)((unsigned)t - before), b, 64));
+    return own >= 0;
+  }
+  auto sum = [&](int level) __attribute__((always_inline)) { return wave_total(min(mine, level)); };
+  int level = 0;  // the largest with S(level) <= t
+  for (int bit = a.level_bits; bit; bit >>= 1)
+    if (sum(level + bit) <= t) level += bit;
+  const unsigned long long have = __ballot(mine > level);
+  const int j = t - sum(level);
+  if (j < 0 || j >= (int)__popcll(have)) return false;
+  const int rank = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(have >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)have, 0));
+  const unsigned long long it = __ballot(mine > level && rank == j);
+  b = __builtin_amdgcn_readfirstlane((int)__ffsll((long long)it) - 1);
+  own = __builtin_amdgcn_readfirstlane(__shfl(mine, b, 64)) - 1 - level;
+  return true;
+}
+// More requests: one after another, by a scan of all threads. place has two ints.
+__device__ __forceinline__ bool find_tile_many(const PagedPrefillArgs& a, unsigned t, int& b, int& own, int* place,
+                                               unsigned* wsum) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int per = (a.B + kNT - 1) / kNT;
   const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
@@ -75,7 +134,7 @@ __device__ __forceinline__ bool find_tile(const PagedPrefillArgs& a, unsigned t,
       const unsigned n = (unsigned)tiles_of(a, x);
       if (t - before < n) {
         place[0] = x;
-        place[1] = (int)(t - before);
+        place[1] = (int)(n - 1 - (t - before));
         break;
       }
       before += n;
@@ -99,7 +158,7 @@ struct Gather {
 
 typedef const __attribute__((address_space(1))) void global_void;
 
-// The first key whose page is not one of the pool's, of those that this lane met.
+// The pages of the key rows that this lane loads of tile kt.
 template <class P>
 __device__ __forceinline__ void look_up(const PagedPrefillArgs& a, const int32_t* row, int kt, int w, int lane, int jlast,
                                         int (&id)[Gather<P>::ROWS]) {
@@ -110,28 +169,50 @@ __device__ __forceinline__ void look_up(const PagedPrefillArgs& a, const int32_t
     id[s] = row[min(kt * kBK + r, jlast) >> a.c.shift];
   }
 }
+// One segment of a row's channels that the cache has; the others' places hold zeros from the start. The instruction's
+// own offset, the segment's 64 bytes of the row, counts at both ends.
+template <class P, int S>
+__device__ __forceinline__ void load_segment(const PagedPrefillArgs& a, const char* k, const char* v, int w, int lane,
+                                             unsigned char* Kd, unsigned char* Vd, int gbyte0) {
+  int r, gbyte, lds_off;
+  P::seg_map(Gather<P>::seg(w, S), lane, r, gbyte, lds_off);
+  constexpr int off = Gather<P>::kOneRow ? 64 * S : 0;
+  if (gbyte0 + off < a.c.D * (int)sizeof(typename P::T)) {
+    __builtin_amdgcn_global_load_lds((global_void*)k, (lds_void*)(Kd + (lds_off - off)), 16, off, 0);
+    __builtin_amdgcn_global_load_lds((global_void*)v, (lds_void*)(Vd + (lds_off - off)), 16, off, 0);
+  }
+}
+// All of a lane's segments of a tile. bad: the first key whose page is not one of the pool's, of those that it met.
+template <class P, int S = 0>
+__device__ __forceinline__ void load_segments(const PagedPrefillArgs& a, const char* k, const char* v, int kt, int w,
+                                              int lane, int jlast, const int (&id)[Gather<P>::ROWS], unsigned char* Kd,
+                                              unsigned char* Vd, int& bad) {
+  if constexpr (S < Gather<P>::SEGW) {
+    int r, gbyte, lds_off;
+    P::seg_map(Gather<P>::seg(w, S), lane, r, gbyte, lds_off);
+    const int j = min(kt * kBK + r, jlast), x = id[Gather<P>::kOneRow ? 0 : S];
+    const bool ok = (unsigned)x < (unsigned)a.c.num_pages;
+    if (!ok) bad = min(bad, j);
+    const int64_t off = ((int64_t)(ok ? x : 0) * a.c.sp + (int64_t)((j & ((1 << a.c.shift) - 1)) * a.c.st)) *
+                            (int64_t)sizeof(typename P::T) + gbyte;
+    if constexpr (Gather<P>::kOneRow) {  // the same row, 64 bytes on
+      const char *kr = k + off, *vr = v + off;
+      load_segment<P, 0>(a, kr, vr, w, lane, Kd, Vd, gbyte);
+      if constexpr (Gather<P>::SEGW > 1) load_segment<P, 1>(a, kr, vr, w, lane, Kd, Vd, gbyte);
+      if constexpr (Gather<P>::SEGW > 2) load_segment<P, 2>(a, kr, vr, w, lane, Kd, Vd, gbyte);
+      if constexpr (Gather<P>::SEGW > 3) load_segment<P, 3>(a, kr, vr, w, lane, Kd, Vd, gbyte);
+    } else {
+      load_segment<P, S>(a, k + off, v + off, w, lane, Kd, Vd, gbyte);
+      load_segments<P, S + 1>(a, k, v, kt, w, lane, jlast, id, Kd, Vd, bad);
+    }
+  }
+}
 template <class P>
 __device__ __forceinline__ void load_tile(const PagedPrefillArgs& a, const char* k, const char* v, int kt, int w, int lane,
                                           int jlast, const int (&id)[Gather<P>::ROWS], unsigned char* Kd,
                                           unsigned char* Vd, int& bad) {
-  constexpr int es = sizeof(typename P::T);
-  const int mask = (1 << a.c.shift) - 1;
-  int64_t off = 0;
-#pragma unroll
-  for (int s = 0; s < Gather<P>::SEGW; ++s) {
-    int r, gbyte, lds_off;
-    P::seg_map(Gather<P>::seg(w, s), lane, r, gbyte, lds_off);
-    if (!Gather<P>::kOneRow || s == 0) {
-      const int j = min(kt * kBK + r, jlast), x = id[Gather<P>::kOneRow ? 0 : s];
-      const bool ok = x >= 0 && x < a.c.num_pages;
-      if (!ok) bad = min(bad, j);
-      off = ((int64_t)(ok ? x : 0) * a.c.sp + (int64_t)(j & mask) * a.c.st) * es;
-    }
-    if (gbyte < a.c.D * es) {  // channels that the cache has; the others' places hold zeros from the start
-      __builtin_amdgcn_global_load_lds((global_void*)(k + off + gbyte), (lds_void*)(Kd + lds_off), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_void*)(v + off + gbyte), (lds_void*)(Vd + lds_off), 16, 0, 0);
-    }
-  }
+  static_assert(!Gather<P>::kOneRow || Gather<P>::SEGW <= 4, "segments of a row");
+  load_segments<P>(a, k, v, kt, w, lane, jlast, id, Kd, Vd, bad);
 }
 
 // The query operand of one row, zero past the cache's width (times c in mode 1).
@@ -361,10 +442,12 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
   const Lane L(lane);
   Tile t;
   int item, own;
-  if (!map_tile(a.map, blockIdx.x, t.h, item, true)) return;
+  if (!map_tile(a.map, blockIdx.x, t.h, item, false)) return;
   t.slice = item / a.tiles;
   if (tid == 0) bad_key = kNone;
-  if (!find_tile(a, (unsigned)(item - t.slice * a.tiles), t.b, own, place, wsum)) return;
+  if (a.B <= 64 ? !find_tile_64(a, item - t.slice * a.tiles, t.b, own)
+                   : !find_tile_many(a, (unsigned)(item - t.slice * a.tiles), t.b, own, place, wsum))
+    return;
   t.n = tokens_of(a, t.b, t.first);
   t.len = a.lengths[t.b];
   t.row0 = own * a.tile_rows;
@@ -504,69 +587,128 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
   if (any) scan_again<P, D>(a, t, redo, bad_key, KA, VA, KB, VB);
 }
 
-// The slices of each row joined, with its Self entry, by one wave: lane holds channels lane and lane + 64.
-template <typename TI>
+// The slices of each row joined, with its Self entry (eqs. 12-13), by 16 lanes of 8 channels each: what is the same for
+// all channels of a row, most of the work, is done for four rows by one instruction. (A wave a row: 26 us against 13 for
+// 25216 rows x 128 of four slices.)
+template <class P>
 __global__ __launch_bounds__(kNT) void prefill_merge_kernel(PagedPrefillArgs a) {
-  constexpr int kBatch = 4;
-  const int64_t rows = (int64_t)a.N * a.Hq, at = (int64_t)blockIdx.x * (kNT / 64) + (threadIdx.x >> 6);
-  if (at >= rows) return;
-  const int lane = threadIdx.x & 63;
-  const int tok = (int)(at / a.Hq), hq = (int)(at - (int64_t)tok * a.Hq);
-  int b = 0;  // requests that end before the token
-  for (int x = 0; x < a.B; x += 64) {
-    const bool ends = x + lane < a.B && a.row_start[x + lane + 1] <= tok;
-    b += (int)__popcll(__ballot(ends));
-  }
-  if (b >= a.B) return;
-  int first;
-  const int n = tokens_of(a, b, first), len = a.lengths[b];
-  if (tok < first || tok >= first + n) return;  // a token of no request
-  const int pos = len >= n && len <= a.max_len ? len - n + tok - first : -1;
-  const SelfEntry self = read_self<TI>(a, b, at, hq, pos + 1, lane);
-  const int D = a.c.D, ns = pos > 0 ? (pos - 1) / a.slice + 1 : 0;  // slices with an Exchange key
-  const int c0 = lane < D ? lane : 0, c1 = lane + 64 < D ? lane + 64 : 0;
-  float m = 0.0f, l = 0.0f, z[2] = {0.0f, 0.0f};
-  for (int s0 = 0; s0 < ns; s0 += kBatch) {
-    float2 ml[kBatch];
-    float zo[kBatch][2];
+  using TI = typename P::T;
+  constexpr int kLanes = 16, kBatch = 4;
+  const int64_t rows = (int64_t)a.N * a.Hq, mine = (int64_t)blockIdx.x * (kNT / kLanes) + threadIdx.x / kLanes;
+  const int64_t at = min(mine, rows - 1);  // whole waves reach the lane moves
+  const int sub = threadIdx.x & (kLanes - 1), D = a.c.D, c0 = 8 * sub;
+  // the first states are on their way while the row's request is looked up; those that nobody wrote count for nothing
+  float2 ml[kBatch], zo[kBatch][4];
+  auto load = [&](int s0, int last) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {  // past the end: the last state again, which counts for nothing
-      const float* st = a.states + ((int64_t)min(s0 + u, ns - 1) * rows + at) * (D + 2);
+    for (int u = 0; u < kBatch; ++u) {
+      const float* st = a.states + ((int64_t)min(s0 + u, last) * rows + at) * (D + 2);  // 8-byte aligned
       ml[u] = *reinterpret_cast<const float2*>(st);
-      zo[u][0] = st[2 + c0];
-      zo[u][1] = st[2 + c1];
-    }
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (s0 + u < ns) merge_into<2>(m, l, z, ml[u].x, ml[u].y, zo[u]);
+      for (int i = 0; i < 4; ++i) {
+        zo[u][i] = float2{0.0f, 0.0f};
+        if (c0 + 2 * i < D) zo[u][i] = *reinterpret_cast<const float2*>(st + 2 + c0 + 2 * i);
+      }
+    }
+  };
+  load(0, a.nsplit - 1);
+  const int tok = (int)(at / a.Hq), hq = (int)(at - (int64_t)tok * a.Hq);
+  // the number of requests that end at or before the token: 16 places of their ends at a time
+  int b = 0;
+#pragma unroll
+  for (int step = 256; step; step /= 16) {
+    const int i = b + (sub + 1) * step;
+    const unsigned long long end = __ballot(i <= a.B && a.row_start[min(i, a.B)] <= tok);
+    b += step * (int)__popc((unsigned)(end >> (threadIdx.x & 48)) & 0xffffu);
   }
-  finish_row<TI>(a, at, pos + 1, lane, self, m, l, z[0], z[1]);
+  int first = 0, n = 0, pos = -1;
+  const int bb = min(b, a.B - 1);
+  n = tokens_of(a, bb, first);
+  const bool is = b < a.B && tok >= first && tok < first + n && mine < rows;  // else a token of no request
+  const int len = a.lengths[bb];
+  if (is && len >= n && len <= a.max_len) pos = len - n + tok - first;
+  // Self
+  int64_t off = 0;
+  const bool ok = pos >= 0 && entry_offset(a, bb, hq / a.G, pos, off);
+  floatx4 v[2] = {};
+  float dot = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {  // widths are multiples of 4
+    if (ok && c0 + 4 * i < D) {
+      const floatx4 x = P::load4((const TI*)a.q + at * D + c0 + 4 * i), y = P::load4((const TI*)a.k + off + c0 + 4 * i);
+      v[i] = P::load4((const TI*)a.v + off + c0 + 4 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(x[e], y[e], dot);
+    }
+  }
+  dot = lane_group_sum<kLanes>(dot);
+  const int ns = pos > 0 ? (pos - 1) / a.slice + 1 : 0;  // slices with an Exchange key
+  float m = 0.0f, l = 0.0f, z[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = 0.0f;
+  for (int s0 = 0; s0 < ns; s0 += kBatch) {
+    if (s0) load(s0, ns - 1);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (s0 + u >= ns) break;
+      const float zu[8] = {zo[u][0].x, zo[u][0].y, zo[u][1].x, zo[u][1].y, zo[u][2].x, zo[u][2].y, zo[u][3].x, zo[u][3].y};
+      merge_into<8>(m, l, z, ml[u].x, ml[u].y, zu);
+    }
+  }
+  if (!is) return;
+  const float lam = *a.lambda, ln_i = logf((float)(pos + 1));
+  const RowEpilogue ep = row_epilogue(m, l, dot * a.scale * kLog2e, a.inv_tau, lam, ln_i);
+  const bool lost = !ok || l != l;  // a bad length, a page outside the pool, or a NaN among the keys
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    floatx4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = lost ? __builtin_nanf("") : __builtin_fmaf(ep.omg, v[i][e], ep.inv_l * z[4 * i + e]);
+    if (c0 + 4 * i < D) P::store4((TI*)a.out + at * D + c0 + 4 * i, y);
+  }
+  if (sub == 0 && a.row_stat) a.row_stat[at] = lost ? __builtin_nanf("") : ep.lnZ + lam * ln_i;
 }
 
 template <class P, int D>
 hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
   a.tiles = (int)((int64_t)a.N * a.G / a.tile_rows + a.B);  // each request has one that is not whole
   a.map = make_tilemap(a.c.H, a.tiles * a.nsplit);
+  a.level_bits = 0;
+  if (a.B <= 64 && (int64_t)a.max_len * a.B <= 2 * (int64_t)a.N)
+    for (a.level_bits = 1; 2 * a.level_bits <= a.tiles; a.level_bits *= 2) {
+    }
   hipLaunchKernelGGL((prefill_kernel<P, D>), dim3((unsigned)grid_size(a.map)), dim3(kNT), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int64_t rows = (int64_t)a.N * a.Hq;
-  hipLaunchKernelGGL((prefill_merge_kernel<typename P::T>), dim3((unsigned)((rows + kNT / 64 - 1) / (kNT / 64))), dim3(kNT), 0,
+  using M = std::conditional_t<sizeof(typename P::T) == 2, PolBF16<32>, PolF32<32>>;  // its loads and stores, of any width
+  hipLaunchKernelGGL((prefill_merge_kernel<M>), dim3((unsigned)((rows + kNT / 16 - 1) / (kNT / 16))), dim3(kNT), 0,
                      stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
+// * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short: one prompt of 2048
+//   tokens, 8 heads x 64, 29 us against 42; five chunks of 151 to 301 after up to 777, 8 heads x 80 in fp32, 98 against 327. With
+//   longer histories the keys that every tile reads again cost more than the slices of 128-row tiles: a chunk of 64
+//   tokens after 16384, 8 heads x 64, 29 us (32 slices), 274 unsplit.
+// * As many slices as bring the workgroups to what the chip holds at once (three workgroups a CU for bf16 of up to 64
+//   channels, else two), each of 512 keys or more: a chunk of 2048 after 32768, 16 heads on 4 x 128, 687 to 716 us
+//   in two slices, 903 to 927 in one, 683 to 706 in four; 7 chunks of 128 to 256 after up to 4096 78 in four, 124 in one. Tiles of 32 rows
+//   that give every CU one are not split: what a merge costs (13 us for 25216 rows of four slices) is more than is won.
 PrefillPlan paged_prefill_plan(int64_t N, int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype) {
-  constexpr int64_t kTarget = 1024, kMinSlice = 512;
+  constexpr int64_t kMinSlice = 512;
+  const int64_t kTarget = dtype == 1 && D <= 64 ? 768 : 512;  // what the chip holds at once
   PrefillPlan p;
   auto groups = [&](int64_t rows) { return (N * G / rows + B) * H; };
-  p.tile_rows = groups(kRows) <= 256 && max_len <= 2048 ? kFewRows : kRows;
-  int64_t split = (kTarget + groups(p.tile_rows) - 1) / groups(p.tile_rows);
+  p.tile_rows = groups(kRows) <= 256 && max_len <= 4096 ? kFewRows : kRows;
+  const int64_t have = groups(p.tile_rows);
+  int64_t split = p.tile_rows == kFewRows && have >= 256 ? 1 : (kTarget + have - 1) / have;
   const int64_t most = (max_len + kMinSlice - 1) / kMinSlice;
   if (split > most) split = most;
-  /*TUNE*/
   int64_t slice = (max_len + split - 1) / split;
   slice = (slice + 2 * kBK - 1) / (2 * kBK) * (2 * kBK);  // pairs of tiles
   p.slice = (int)slice;
@@ -584,6 +726,7 @@ hipError_t launch_paged_prefill(const PagedPrefillArgs& a, int dtype, hipStream_
   }
   if (D <= 32) return launch_one<PolF32<32>, 32>(a, stream);
   if (D <= 64) return launch_one<PolF32<64>, 64>(a, stream);
+  if (D <= 96) return launch_one<PolF32<128>, 96>(a, stream);  // rows as for 128, three quarters of the products
   return launch_one<PolF32<128>, 128>(a, stream);
 }
 

@@ -158,6 +158,57 @@ def test_prefill_sharp(dtype, G):
     _close(_run(s, 2.0, scale=0.3, tau_s=0.5, max_length=640), s, dtype, 2.0, scale=0.3, tau_s=0.5)
 
 
+@pytest.mark.parametrize("chunks,H,G,D,page,dtype", [
+    ([(5000, 40)], 2, 1, 64, 16, "bf16"), ([(9000, 3), (100, 200), (4097, 1)], 1, 4, 128, 32, "bf16"), ([(4200, 130)], 3, 2, 48, 8, "bf16"),
+    ([(4400, 33), (5, 5)], 1, 3, 80, 16, "f32"), ([(6000, 1)] * 3, 2, 2, 120, 64, "f32"), ([(4700, 300)], 1, 1, 32, 1, "bf16"),
+    ([(700, 20)], 1, 1, 4, 4, "f32"), ([(2500, 8), (1, 1)], 2, 1, 24, 16, "bf16"), ([(513, 1), (512, 1), (511, 2), (1024, 1)], 1, 1, 64, 16, "bf16"),
+    ([(4500, 60)], 2, 1, 100, 16, "f32"), ([(8000, 1)] * 70, 1, 1, 32, 128, "bf16"),
+])
+def test_prefill_long_histories(chunks, H, G, D, page, dtype):
+    """Few rows over many keys: the history in slices, joined by a second kernel; rows whose history ends in any slice."""
+    log(f"[prefill] slices {chunks[:4]} H={H} G={G} D={D} page={page} {dtype}")
+    s = _step(chunks, H, G, D, page, dtype)
+    c, d = R.make_pages(s["kc"], s["vc"]), R.RelPagedChunk(s["q"].shape[0], len(chunks), H * G, s["table"].shape[1], 0, 2.0, 0.0)
+    assert R.load_library().relation_paged_prefill_workspace_bytes(R.ctypes.byref(c), R.ctypes.byref(d)) > 0  # several slices
+    r = _run(s)
+    _close(r, s, dtype, most=12)
+    ws = torch.full((1 << 24,), 255, dtype=torch.uint8, device=DEV)  # states that nobody writes are NaN there
+    again = _run(s, workspace=ws)
+    assert torch.equal(r["o"], again["o"]) and torch.equal(r["row_stat"], again["row_stat"])
+
+
+@pytest.mark.parametrize("dtype,D,G,n", [("bf16", 64, 1, 40), ("bf16", 128, 4, 50), ("f32", 80, 2, 3)])
+def test_prefill_slices_that_are_scanned_again(dtype, D, G, n):
+    """Totals past 2^64 in some slices, values that are not finite behind rows and in their history, and bad pages: in
+    the slices where they are."""
+    chunks = [(4600, n), (4300, 2)]
+    s = _step(chunks, 2, G, D, 16, dtype, std=4.0)
+    _close(_run(s), s, dtype, most=12)
+    s = _step(chunks, 2, G, D, 16, dtype)
+    base = _run(s)
+    at = 4600 + n - 2  # the last row but one: it and the last row have the entry
+    for value in (math.nan, math.inf):
+        t = {**s, "vc": s["vc"].clone()}
+        t["vc"][s["table"][0, at // 16], 1, at % 16, 3] = value
+        r = _run(t)
+        o, w = r["o"].view(-1, 2, G, D), base["o"].view(-1, 2, G, D)
+        assert torch.equal(o[:, 0], w[:, 0]) and torch.equal(o[n:], w[n:])
+        assert rel_l2(_np(o[:n - 2]), _np(w[:n - 2])) <= BAR[dtype] if n > 2 else True
+        assert not torch.isfinite(o[n - 2:n, 1, :, 3]).any()
+        t["vc"][s["table"][0, 100 // 16], 0, 100 % 16, 5] = value  # far back: all rows of the head
+        r = _run(t)
+        assert not torch.isfinite(r["o"].view(-1, 2, G, D)[:n, 0, :, 5]).any() and torch.isfinite(r["o"][n:]).all()
+        assert torch.isfinite(r["row_stat"]).all()
+    P = s["kc"].shape[0]
+    t = {**s, "table": s["table"].copy()}
+    t["table"][1, 10] = P
+    if n > 8:  # the first row's page is the one before
+        t["table"][0, 4600 // 16 + 1] = -1
+    r = _run(t)
+    _close(r, t, dtype, most=12)
+    assert torch.isnan(r["row_stat"][n:]).all() and not torch.isnan(r["row_stat"][0]).any()
+
+
 def test_prefill_is_decode_a_token_at_a_time():
     """Every row of the chunk as relation_paged_decode gives it at that length."""
     s = _step([(300, 40), (0, 23)], 4, 2, 64, 16, "bf16", "nhd")
