@@ -2,17 +2,20 @@
 """Generate tokens for several requests from one paged cache.
 
 A small Relation decoder with random weights takes in prompts of different
-lengths and then decodes them together, one token each a step:
+lengths, whole or in chunks, and then decodes them together, one token each a step:
 
-  relation_page_map      pages and slots of the step's tokens, from lengths on the GPU
-  relation_paged_append  RoPE on q and k, Givens mixing of v, rows into the pages
-  relation_paged_decode  Full Relation of the new rows over the pages (prompts: relation_layer_fwd)
-  relation_sample        the next tokens from the logits
+  relation_page_map        pages and slots of the step's tokens, from lengths on the GPU
+  relation_qk_norm_fwd     RMS norm of the heads of q and k and RoPE (--norm)
+  relation_paged_append    RoPE on q and k without --norm, Givens mixing of v, rows into the pages
+  relation_paged_prefill   Full Relation of the prompts' rows over the pages
+  relation_paged_decode    the same of one new row of each request
+  relation_token_logprobs_fwd  log-probability and rank of the prompts' own tokens
+  relation_sample          the next tokens from the logits
 
 Every layer has its own pools; the block tables are shared. The host keeps count
 of what it asks for and reads nothing back but the finished tokens.
 
-  python examples/serve_paged.py [--steps N] [--check]
+  python examples/serve_paged.py [--steps N] [--chunk N] [--norm] [--check]
 
 --check replays the finished sequences through relation_layer_fwd and compares
 the last hidden rows with those of the decode steps.
@@ -31,9 +34,10 @@ from paper_2608_20172_amd import binding as R  # noqa: E402
 
 
 class Decoder:
-    """Layers of norm, q/k/v projections, Relation and an output projection, with a residual; random weights."""
+    """Layers of norm, q/k/v projections, Relation and an output projection, with a residual; random weights. With
+    head_norm, q and k have an RMS norm of every head, with weights, before the rotation."""
 
-    def __init__(self, vocab=5000, layers=2, heads=8, width=64, seed=0, dev="cuda"):
+    def __init__(self, vocab=5000, layers=2, heads=8, width=64, seed=0, dev="cuda", head_norm=False):
         g = torch.Generator(device=dev).manual_seed(seed)
         dim = heads * width
         mat = lambda n, m: (torch.randn(n, m, device=dev, generator=g) / n ** 0.5).to(torch.bfloat16)
@@ -44,6 +48,8 @@ class Decoder:
         self.lam = [torch.full((1,), 0.5, device=dev) for _ in range(layers)]
         self.theta = [(torch.rand(heads // 2, device=dev, generator=g) * 2 - 1) for _ in range(layers)]
         self.pairing = ["A" if n % 2 == 0 else "B" for n in range(layers)]
+        weight = lambda: 1 + 0.3 * torch.randn(width, device=dev, generator=g)
+        self.head_norms = [(weight(), weight()) for _ in range(layers)] if head_norm else None
 
     def qkv(self, n, x):
         """q, k, v [N, H, D] of x [N, dim]."""
@@ -56,6 +62,9 @@ class Decoder:
         x = self.emb[tokens]
         for n in range(self.layers):
             q, k, v = (t.transpose(0, 1)[None] for t in self.qkv(n, x))
+            if self.head_norms:
+                f = R.relation_qk_norm_fwd(q, k, *self.head_norms[n], rope_dim=0)
+                q, k = f["q"], f["k"]
             o = R.relation_layer_fwd(q, k, v, self.lam[n], self.theta[n], pairing=self.pairing[n])["o"]
             x = x + o[0].transpose(0, 1).reshape(-1, self.dim) @ self.wo[n]
         return x
@@ -91,34 +100,63 @@ class Pool:
         return m
 
 
+def new_rows(model, pool, m, x, one_each, longest):
+    """Hidden rows [N, dim] of a step's tokens (x: their embeddings), whose keys and values go into the pages; one_each:
+    the step has one token of every request."""
+    for n in range(model.layers):
+        q, k, v = model.qkv(n, x)
+        base = R.ROPE_BASE
+        if model.head_norms:
+            f = R.relation_qk_norm_fwd(q, k, *model.head_norms[n], m["positions"])
+            q, k, base = f["q"], f["k"], None
+        caches = pool.caches(n)
+        q = R.relation_paged_append(k, v, *caches, m["slots"], m["positions"], q=q, theta=model.theta[n],
+                                    pairing=model.pairing[n], rope_base=base)
+        over = (m["lengths"],) if one_each else (m["lengths"], m["row_start"])
+        f = (R.relation_paged_decode if one_each else R.relation_paged_prefill)(
+            q, *caches, pool.table, *over, model.lam[n], max_length=longest, head_dim=model.D)
+        x = x + f["o"][:, :, :model.D].reshape(-1, model.dim) @ model.wo[n]
+    return x
+
+
+def take_in(model, pool, prompts, longest, chunk=None):
+    """The prompts, up to `chunk` tokens of each a step: the hidden rows [T, dim] of each."""
+    rows, at = [[] for _ in prompts], 0
+    while at < max(len(p) for p in prompts):
+        part = [p[at:at + (chunk or longest)] for p in prompts]
+        added = [len(p) for p in part]
+        x = new_rows(model, pool, pool.step(added), model.emb[torch.cat(part)], False, longest)
+        for r, y in zip(rows, x.split(added)):
+            r.append(y)
+        at += max(added)
+    return [torch.cat(r) for r in rows]
+
+
+def score(model, prompts, rows):
+    """Log-probability and rank [T - 1] of the tokens 1 .. T-1 of each prompt, from its hidden rows."""
+    tokens = torch.cat([torch.cat([p[1:], p.new_full((1,), -1)]) for p in prompts])  # -1: none given after the last
+    f = R.relation_token_logprobs_fwd(torch.cat(rows) @ model.head, tokens, want_rank=True)
+    at = [len(p) for p in prompts]
+    return [(a[:-1], b[:-1]) for a, b in zip(f["logprob"].split(at), f["rank"].split(at))]
+
+
 def sample(model, x, g, filters):
     logits = x @ model.head
     noise = torch.empty(logits.shape, device=logits.device).exponential_(generator=g)
     return R.relation_sample(logits, noise, **filters)
 
 
-def generate(model, prompts, steps, *, page_size=16, seed=1, **filters):
-    """Token ids [B, steps], their logprobs, and the hidden rows [B, dim] of the last step."""
+def generate(model, prompts, steps, *, page_size=16, seed=1, chunk=None, scores=None, **filters):
+    """Token ids [B, steps], their logprobs, and the hidden rows [B, dim] of the last step. scores: a list that gets each
+    prompt's own log-probabilities and ranks."""
     dev, B = model.emb.device, len(prompts)
     g = torch.Generator(device=dev).manual_seed(seed)
     longest = max(len(p) for p in prompts) + steps
     pool = Pool(model, B, sum(-(-(len(p) + steps) // page_size) for p in prompts), page_size, longest)
-    # prompts: their rows by the whole-sequence operator, their keys and values into the pages
-    m = pool.step([len(p) for p in prompts])
-    ends = torch.tensor([len(p) for p in prompts], device=dev).cumsum(0)
-    x = model.emb[torch.cat(prompts)]
-    for n in range(model.layers):
-        q, k, v = model.qkv(n, x)
-        R.relation_paged_append(k, v, *pool.caches(n), m["slots"], m["positions"], theta=model.theta[n],
-                                pairing=model.pairing[n])
-        rows, at = [], 0
-        for p in prompts:
-            part = [t[at:at + len(p)].transpose(0, 1)[None] for t in (q, k, v)]
-            o = R.relation_layer_fwd(*part, model.lam[n], model.theta[n], pairing=model.pairing[n])["o"]
-            rows.append(o[0].transpose(0, 1).reshape(-1, model.dim))
-            at += len(p)
-        x = x + torch.cat(rows) @ model.wo[n]
-    x = x[ends - 1]
+    rows = take_in(model, pool, prompts, longest, chunk)
+    if scores is not None:
+        scores += score(model, prompts, rows)
+    x = torch.stack([r[-1] for r in rows])
     out, logprob = [], []
     for step in range(steps):
         s = sample(model, x, g, filters)
@@ -126,15 +164,7 @@ def generate(model, prompts, steps, *, page_size=16, seed=1, **filters):
         logprob.append(s["logprob"])
         if step + 1 == steps:
             break
-        m = pool.step([1] * B)
-        x = model.emb[s["tokens"]]
-        for n in range(model.layers):
-            q, k, v = model.qkv(n, x)
-            q = R.relation_paged_append(k, v, *pool.caches(n), m["slots"], m["positions"], q=q, theta=model.theta[n],
-                                        pairing=model.pairing[n])
-            o = R.relation_paged_decode(q, *pool.caches(n), pool.table, m["lengths"], model.lam[n], max_length=longest,
-                                        head_dim=model.D)["o"]
-            x = x + o[:, :, :model.D].reshape(B, model.dim) @ model.wo[n]
+        x = new_rows(model, pool, pool.step([1] * B), model.emb[s["tokens"]], True, longest)
     return torch.stack(out, 1), torch.stack(logprob, 1), x
 
 
@@ -150,14 +180,18 @@ def check(model, prompts, tokens, x):
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--steps", type=int, default=40)
+    ap.add_argument("--chunk", type=int, help="take the prompts in by chunks of so many tokens")
+    ap.add_argument("--norm", action="store_true", help="RMS norm of the heads of q and k")
     ap.add_argument("--check", action="store_true")
     a = ap.parse_args()
-    model = Decoder()
+    model = Decoder(head_norm=a.norm)
     g = torch.Generator(device="cuda").manual_seed(3)
     prompts = [torch.randint(0, model.emb.shape[0], (n,), device="cuda", generator=g) for n in (1, 7, 16, 45, 130, 300)]
-    tokens, logprob, x = generate(model, prompts, a.steps, temperature=0.8, top_k=50, top_p=0.9)
-    for p, t, l in zip(prompts, tokens.tolist(), logprob.mean(1).tolist()):
-        print(f"prompt of {len(p):4d}: {' '.join(map(str, t[:10]))} ...  mean logprob {l:.3f}")
+    scores = []
+    tokens, logprob, x = generate(model, prompts, a.steps, chunk=a.chunk, scores=scores, temperature=0.8, top_k=50, top_p=0.9)
+    for p, t, l, (own, rank) in zip(prompts, tokens.tolist(), logprob.mean(1).tolist(), scores):
+        of_its_own = f", its own {own.mean():.3f}, best rank {int(rank.min())}" if len(p) > 1 else ""
+        print(f"prompt of {len(p):4d}: {' '.join(map(str, t[:10]))} ...  mean logprob {l:.3f}{of_its_own}")
     if a.check:
         err = check(model, prompts, tokens, x)
         print(f"last hidden rows against whole sequences: relative 2-norm {err:.2e}")

@@ -692,13 +692,13 @@ hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
 
 // Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
 // * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short: one prompt of 2048
-//   tokens, 8 heads x 64, 29 us against 42; five chunks of 151 to 301 after up to 777, 8 heads x 80 in fp32, 98 against 327. With
-//   longer histories the keys that every tile reads again cost more than the slices of 128-row tiles: a chunk of 64
-//   tokens after 16384, 8 heads x 64, 29 us (32 slices), 274 unsplit.
-// * As many slices as bring the workgroups to what the chip holds at once (three workgroups a CU for bf16 of up to 64
-//   channels, else two), each of 512 keys or more: a chunk of 2048 after 32768, 16 heads on 4 x 128, 687 to 716 us
-//   in two slices, 903 to 927 in one, 683 to 706 in four; 7 chunks of 128 to 256 after up to 4096 78 in four, 124 in one. Tiles of 32 rows
-//   that give every CU one are not split: what a merge costs (13 us for 25216 rows of four slices) is more than is won.
+//   tokens, 8 heads x 64, 29 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 98
+//   against 327. With longer histories the keys that every tile reads again cost more than slices of 128-row tiles: a
+//   chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
+// * As many slices as bring the workgroups to what the chip holds at once (three a CU for bf16 of up to 64 channels,
+//   else two), each of 512 keys or more: a chunk of 2048 after 32768, 16 heads on 4 x 128, 687 to 716 us in two slices,
+//   903 to 927 in one, 683 to 706 in four; 7 chunks of 128 to 256 after up to 4096 78 in four, 124 in one. Tiles of 32
+//   rows that give every CU one are not split: a merge costs more than is won (13 us for 25216 rows of four slices).
 PrefillPlan paged_prefill_plan(int64_t N, int64_t B, int64_t H, int64_t G, int64_t max_len, int D, int dtype) {
   constexpr int64_t kMinSlice = 512;
   const int64_t kTarget = dtype == 1 && D <= 64 ? 768 : 512;  // what the chip holds at once
