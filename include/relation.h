@@ -552,7 +552,8 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  * that bound gets NaN rows, and so does a row if a page of its entries is not in the
  * pool. Entries past a request's length are not read; NaN and infinities in the
  * entries after a row do not reach it. An infinite value among a row's own entries
- * may come out as NaN in its channel. B at most 4096, N at most 2^26, N Hq at most 2^30. */
+ * may come out as NaN in its channel. B at most 4096, B H at most 2^22, N at most 2^26, N Hq at most
+ * 2^30. */
 typedef struct rel_paged_chunk {
   int64_t N, B, Hq, table_width, max_length;
   float tau_s, scale; /* as in rel_paged_query */
@@ -619,7 +620,7 @@ rel_status relation_sample(const rel_sample* s, const void* logits, const float*
  *              all); NULL: 0 .. T-1. A token at a negative position belongs to
  *              nobody: its output rows are 0, and so are its gradients.
  *   D <= 128; rope_dim even, 0 (no rotation) .. D; rope_base > 1.
- * Angles are formed in 64 bits, sums in 32; each output is rounded once. NaN and
+ * At most 2^26 tokens and 2^16 heads. Angles are formed in 64 bits, sums in 32; each output is rounded once. NaN and
  * infinities stay in their row (in the backward pass also in the weights' gradients). */
 typedef enum rel_rope_layout {
   REL_ROPE_HALF = 0,
@@ -674,10 +675,12 @@ rel_status relation_qk_norm_bwd(const rel_qk_norm* p, const void* q, const void*
  *   workspace  relation_token_logprobs_workspace_bytes(p) bytes, 16-byte aligned; it
  *              serves fewer rows as well
  * NaN logits count as -inf; p is 0 at -inf, and below +inf. A row with nothing above
- * -inf has NaN in every fp32 output, rank -1 and top tokens -1.
+ * -inf has NaN in every fp32 output (but for the logprob 0 of a row without a token),
+ * rank -1 and top tokens -1.
  * K <= 32, K <= V <= 2^22, N <= 2^20, N V <= 2^36.
  * Backward: dlogits_i = g ([i = t] - p_i) - h p_i (log p_i + entropy), with
- * g = dlogprob (fp32 [N]; NULL: 0), h = dentropy (the same). dlogits [N, V] dtype,
+ * g = dlogprob (fp32 [N]; NULL: 0), h = dentropy (the same). A row without a token and
+ * with h = 0 is 0 whatever its logits are. dlogits [N, V] dtype,
  * rows stride_grad (at least V) elements apart. */
 typedef struct rel_token_logprobs {
   int64_t N, V, K;

@@ -84,7 +84,7 @@ def logprobs(x, token: int, top: int = 0) -> dict:
     V, m = len(x), x.max()
     nan = math.nan
     if m == -np.inf:
-        return {"logprob": nan, "entropy": nan, "rank": -1, "top_tokens": [-1] * top, "top_logprobs": [nan] * top,
+        return {"logprob": 0.0 if token < 0 else nan, "entropy": nan, "rank": -1, "top_tokens": [-1] * top, "top_logprobs": [nan] * top,
                 "logp": np.full(V, nan), "p": np.full(V, nan)}
     with np.errstate(invalid="ignore"):
         d = np.where(x == m, 0.0, x - m)
@@ -106,6 +106,8 @@ def logprobs_backward(x, token: int, g: float, h: float):
     V = len(p)
     if token >= V:
         return np.full(V, math.nan)
+    if token < 0 and h == 0:
+        return np.zeros(V)  # nothing of the row is asked for
     some = p > 0
     dlogp = np.zeros(V)  # of g logp_t - h sum p logp by logp, with p = exp(logp)
     dlogp[some] = -h * p[some] * (logp[some] + 1.0)

@@ -1234,7 +1234,10 @@ class _QkNormFn(torch.autograd.Function):
 
 
 def relation_qk_norm(q, k, q_weight=None, k_weight=None, positions=None, **opts):
-    """Differentiable relation_qk_norm_fwd (its options): (q, k) normed and rotated, gradients for q, k and the weights."""
+    """Differentiable relation_qk_norm_fwd (its options but ``out``): (q, k) normed and rotated, gradients for q, k and the
+    weights."""
+    if "out" in opts:
+        raise ValueError("out: outputs of their own only")
     return _QkNormFn.apply(q, k, q_weight, k_weight, positions, opts)
 
 

@@ -104,7 +104,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int n, State s, flo
   const int tid = threadIdx.x;
   if (tid == 0) {
     xt = no_nan(xt);
-    const float lp = none || t >= a.V ? nan : t < 0 ? 0.0f : (xt == s.m ? 0.0f : xt - s.m) - ln_z;
+    const float lp = t < 0 ? 0.0f : none || t >= a.V ? nan : (xt == s.m ? 0.0f : xt - s.m) - ln_z;
     if (a.logprob) a.logprob[n] = lp;
     if (a.entropy) a.entropy[n] = H;
     if (a.rank) a.rank[n] = none || t < 0 || t >= a.V ? -1 : s.before;
@@ -542,11 +542,12 @@ __global__ __launch_bounds__(kT) void logprobs_join_kernel(LogprobArgs a, int pa
   finish(a, n, s, xt, first);
 }
 
-// dlogits of one piece of a row a thread and turn.
+// dlogits of one piece of a row a thread. Rows without a token and an entropy gradient are 0 unread, whatever they hold.
 template <typename TI>
-__global__ __launch_bounds__(kT) void logprobs_bwd_kernel(LogprobGradArgs a, int per_row) {
+__global__ __launch_bounds__(kT) void logprobs_bwd_kernel(LogprobGradArgs a, int per_row, int slab) {
   constexpr int VE = Logits<TI>::VE;
-  const int n = blockIdx.x / per_row, c = blockIdx.x % per_row;
+  const int n = blockIdx.y * slab + blockIdx.x / per_row, c = blockIdx.x % per_row;
+  if (n >= a.N) return;
   const TI* row = (const TI*)a.logits + (int64_t)n * a.sl;
   TI* out = (TI*)a.dlogits + (int64_t)n * a.sg;
   const float4 st = *reinterpret_cast<const float4*>(a.stats + 4 * (int64_t)n);
@@ -565,6 +566,14 @@ __global__ __launch_bounds__(kT) void logprobs_bwd_kernel(LogprobGradArgs a, int
   };
   const int at = (c * kT + threadIdx.x) * VE;
   if (at >= a.V) return;
+  if (t < 0 && h == 0.0f) {
+    if (a.V >= VE) {
+      *reinterpret_cast<typename Logits<TI>::V*>(out + min(at, a.V - VE)) = typename Logits<TI>::V{};
+    } else {
+      for (int e = at; e < min(at + VE, a.V); ++e) out[e] = (TI)0.0f;
+    }
+    return;
+  }
   if (a.V >= VE) {
     const int i0 = min(at, a.V - VE);  // the last piece ends with the row: what it shares with the one before is the same
     const typename Logits<TI>::V raw = *reinterpret_cast<const typename Logits<TI>::V*>(row + i0);
@@ -657,11 +666,12 @@ hipError_t launch_logprobs_fwd(const LogprobArgs& a, int dtype, hipStream_t stre
 
 hipError_t launch_logprobs_bwd(const LogprobGradArgs& a, int dtype, hipStream_t stream) {
   const int piece = kT * (dtype == 1 ? 8 : 4), per_row = (a.V + piece - 1) / piece;
-  const dim3 grid((unsigned)((int64_t)a.N * per_row));
+  const int slab = std::min(a.N, (1 << 23) / per_row);  // rows: a grid is under 2^32 threads along x
+  const dim3 grid((unsigned)(slab * per_row), (unsigned)((a.N + slab - 1) / slab));
   if (dtype == 1)
-    hipLaunchKernelGGL((logprobs_bwd_kernel<bf16>), grid, dim3(kT), 0, stream, a, per_row);
+    hipLaunchKernelGGL((logprobs_bwd_kernel<bf16>), grid, dim3(kT), 0, stream, a, per_row, slab);
   else
-    hipLaunchKernelGGL((logprobs_bwd_kernel<float>), grid, dim3(kT), 0, stream, a, per_row);
+    hipLaunchKernelGGL((logprobs_bwd_kernel<float>), grid, dim3(kT), 0, stream, a, per_row, slab);
   return hipGetLastError();
 }
 

@@ -279,6 +279,7 @@ static rel_status check_chunk(const rel_pages* c, const rel_paged_chunk* d, rel_
   if (*empty) return REL_OK;
   if (d->B > rel::kPrefillMaxB)
     return api_fail(REL_ERR_UNSUPPORTED, "%lld requests: at most %d in one chunk step", (long long)d->B, rel::kPrefillMaxB);
+  if (d->B * c->H > (1 << 22)) return api_fail(REL_ERR_UNSUPPORTED, "B * H exceeds 2^22");
   if (d->N > (1 << 26) || d->N * d->Hq > (1 << 30)) return api_fail(REL_ERR_UNSUPPORTED, "over 2^26 tokens or 2^30 rows");
   return REL_OK;
 }

@@ -57,8 +57,8 @@ rel_status check_norm(const rel_qk_norm* p, bool* empty) {
   }
   *empty = p->B == 0 || p->T == 0 || (p->Hq == 0 && p->H == 0);
   if (*empty) return REL_OK;
-  if (p->B > (1 << 30) || p->T > (1 << 30) || p->B * p->T > (1 << 30) || p->Hq > (1 << 16) || p->H > (1 << 16))
-    return api_fail(REL_ERR_UNSUPPORTED, "over 2^30 tokens or 2^16 heads");
+  if (p->B > (1 << 30) || p->T > (1 << 30) || p->B * p->T > (1 << 26) || p->Hq > (1 << 16) || p->H > (1 << 16))
+    return api_fail(REL_ERR_UNSUPPORTED, "over 2^26 tokens or 2^16 heads");
   if (p->position_stride < 0 || (p->position_stride && p->B > 1 && p->position_stride < p->T))
     return api_fail(REL_ERR_INVALID_ARG, "position_stride must be 0 or at least T");
   if (p->B > 1 && p->position_stride > kFarStride / (p->B - 1)) return api_fail(REL_ERR_UNSUPPORTED, "positions span over 2^40");

@@ -63,6 +63,12 @@ def test_chunk_pool(lib, kw, code):
     assert chunk(lib, pages(**kw)) == code
 
 
+def test_chunk_requests_times_heads(lib):
+    """A grid of over 2^32 threads is refused."""
+    for H, code in ((1024, HIP), (1025, UNSUP)):
+        assert chunk(lib, c=pages(P=1, page=1, H=H, D=8), B=4096, Hq=H) == code
+
+
 def test_chunk_pointers(lib):
     for n in ("q", "kc", "vc", "table", "lengths", "start", "lam", "out"):
         assert chunk(lib, **{n: None}) == BAD and chunk(lib, **{n: A[12] + 2}) == BAD
@@ -131,7 +137,7 @@ def norm_bwd(lib, p=None, ws_bytes=1 << 23, **kw):
     (dict(pstride=0), HIP), (dict(pstride=-1), BAD), (dict(pstride=1 << 41), UNSUP), (dict(B=1, pstride=3), HIP), (dict(H=1 << 17), UNSUP),
     (dict(B=1 << 16, T=1 << 16), UNSUP), (dict(q=(-1, 64, 64)), BAD), (dict(q=(0, 0, 0)), HIP), (dict(q_out=(0, 640, 64)), BAD),
     (dict(q_out=(2560, 640, 63)), BAD), (dict(k=(1 << 41, 64, 64)), UNSUP), (dict(k_out=(1 << 40, 1 << 38, 64)), HIP),
-    (dict(Hq=0), HIP), (dict(H=0), HIP),
+    (dict(Hq=0), HIP), (dict(H=0), HIP), (dict(B=1, T=(1 << 26) + 1), UNSUP),
 ])
 def test_norm_sizes(lib, kw, code):
     far = dict(qo=A[9], ko=A[9] + (1 << 43))

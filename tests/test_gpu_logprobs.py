@@ -212,6 +212,42 @@ def test_offsets_past_32_bits():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3, 5000])
+def test_rows_without_a_token_count_for_nothing(V, dtype):
+    """Padding rows, whatever stands there: logprob 0, and a gradient of 0 unless the entropy is asked for."""
+    x = _logits(6, V, dtype, np.random.default_rng(3))
+    x[1], x[2], x[3] = math.nan, -math.inf, math.inf
+    t = torch.tensor([2, -1, -1, -1, -5, 0], device=DEV)
+    leaf = x.clone().requires_grad_()
+    lp, H = R.relation_token_logprobs(leaf, t)
+    assert lp[1:5].tolist() == [0.0] * 4 and torch.isfinite(lp).all()
+    (lp.sum() + torch.where(t >= 0, H, 0.0).sum()).backward()
+    assert not leaf.grad[1:5].any() and torch.isfinite(leaf.grad).all() and leaf.grad[0].any() and leaf.grad[5].any()
+    f = R.relation_token_logprobs_fwd(x, t)
+    g, h = torch.full((6,), math.inf, device=DEV), torch.tensor([0.0, 0.0, 0.0, 0.0, 0.5, 0.0], device=DEV)
+    d = R.relation_token_logprobs_bwd(x, t, f["stats"], g, h)
+    assert not d[1:4].any() and d[4].any() and torch.isfinite(d[4]).all()
+
+
+def test_gradient_of_more_threads_than_a_grid_has():
+    """2^34 gradients in fp32, four a thread: rows of every part of the grid."""
+    N, V = 131200, 131072
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 69 GB")
+    x = _logits(1, V, "f32", np.random.default_rng(4))
+    t = torch.full((N,), 7, device=DEV)
+    f = R.relation_token_logprobs_fwd(x, t[:1])
+    stats, g, h = f["stats"].expand(N, 4).contiguous(), torch.ones(N, device=DEV), torch.ones(N, device=DEV)
+    d = torch.empty((N, V), device=DEV)
+    R.relation_token_logprobs_bwd(x.expand(N, V), t, stats, g, h, out={"dlogits": d})
+    want = R.relation_token_logprobs_bwd(x, t[:1], stats[:1], g[:1], h[:1])[0]
+    for n in (0, 1, 65535, 65536, 131070, 131071, 131072, 131198, 131199):
+        assert torch.equal(d[n], want), n
+    del d
+    torch.cuda.empty_cache()
+
+
 def test_gradients_by_differences_and_through_autograd():
     """Central differences of the forward kernel in fp32 along random directions, step 2^-6: the cubic term is some
     1e-4 of the gradient's size, the rounding of the outputs 1e-5; bar 2e-3."""

@@ -331,3 +331,9 @@ def test_arguments_are_checked():
         R.relation_qk_norm_bwd(x, x, None, None, x, None)
     with pytest.raises(TypeError):
         R.relation_qk_norm_fwd(x.half(), None)
+
+
+def test_outputs_of_the_differentiable_call_are_its_own():
+    q = torch.randn((5, 2, 16), device=DEV)
+    with pytest.raises(ValueError, match="out"):
+        R.relation_qk_norm(q, None, out={"q": torch.empty_like(q)})

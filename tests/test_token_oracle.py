@@ -104,6 +104,8 @@ def test_logprobs_of_known_rows():
     assert r["logprob"] == -math.inf and math.isclose(r["entropy"], math.log(2)) and r["top_tokens"] == [0, 2, 1, 3, 4]
     assert TO.logprobs([1.0, 2.0], -1)["logprob"] == 0.0 and math.isnan(TO.logprobs([1.0, 2.0], 2)["logprob"])
     assert math.isnan(TO.logprobs([-math.inf, math.nan], 0)["entropy"])
+    assert TO.logprobs([-math.inf, math.nan], -1)["logprob"] == 0.0
+    assert not TO.logprobs_backward([-math.inf, math.nan], -1, 2.0, 0.0).any()
 
 
 def test_logprob_gradients_by_differences():
