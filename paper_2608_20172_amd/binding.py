@@ -1235,7 +1235,7 @@ class _QkNormFn(torch.autograd.Function):
 
 def relation_qk_norm(q, k, q_weight=None, k_weight=None, positions=None, **opts):
     """Differentiable relation_qk_norm_fwd (its options but ``out``): (q, k) normed and rotated, gradients for q, k and the
-    weights."""
+    weights. To capture the backward pass into a graph, let no graph of earlier eager calls on the same leaves live."""
     if "out" in opts:
         raise ValueError("out: outputs of their own only")
     return _QkNormFn.apply(q, k, q_weight, k_weight, positions, opts)
@@ -1259,5 +1259,6 @@ class _TokenLogprobsFn(torch.autograd.Function):
 
 
 def relation_token_logprobs(logits, tokens):
-    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]."""
+    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]. To
+    capture the backward pass into a graph, let no graph of earlier eager calls on the same leaves live."""
     return _TokenLogprobsFn.apply(logits, tokens)
