@@ -13,7 +13,7 @@
 //   each wave 32 of every 128 keys instead; the four partial sums meet in LDS. With
 //   the reference at 0 they only add. (40 requests that decode and 8 chunks of 128 to
 //   256 tokens over 410 to 4096 keys, 16 heads of width 128 on 4: 194 us with such a
-//   tile's rows all on one wave, now 117.)
+//   tile's rows all on one wave, now 118.)
 // * Where the tiles leave CUs idle the histories are split into slices whose terminal
 //   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
@@ -29,7 +29,7 @@
 // What bounds it is the vector work of a weight, about 9 instructions a lane and
 // entry beside one matrix instruction, as in the fused forward pass, and the waits
 // of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
-// 704 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 78 us. On
+// 690 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 76 us. On
 // the same rows in one dense tensor the fused forward pass, which looks nothing up,
 // takes 62 us against 73 (8 x 12 x 1536 x 64) and 163 against 199 (4 x 8 x 4096 x 128).
 #include "kernels.h"
@@ -53,12 +53,22 @@ constexpr int kNone = 0x7fffffff;
 
 __device__ __forceinline__ unsigned add_many(unsigned x, unsigned y) { return min(x + y, kMany); }
 
-// Sum over the wave, of numbers whose sum stays under 2^31 for ascending row starts; others wrap, to some place.
+// f over the wave, by every lane: within rows of 16 lanes, then over the rows.
+template <typename F>
+__device__ __forceinline__ int over_wave(int x, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false));
+  return f(f(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)),
+           f(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+// Of numbers whose sum stays under 2^31 for ascending row starts; others wrap, to some place.
 __device__ __forceinline__ int wave_total(int x) {
-  unsigned u = (unsigned)x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) u += __shfl_xor(u, o, 64);
-  return __builtin_amdgcn_readfirstlane((int)(u & 0x7fffffffu));
+  return over_wave(x, [](int y, int z) { return (int)((unsigned)y + (unsigned)z); }) & 0x7fffffff;
+}
+__device__ __forceinline__ int wave_most(int x) {
+  return over_wave(x, [](int y, int z) { return max(y, z); });
 }
 
 // Tokens of request b and the first of them, whatever row_start holds.
@@ -71,59 +81,45 @@ __device__ __forceinline__ int tiles_of(const PagedPrefillArgs& a, int b) {
   return (tokens_of(a, b, first) * a.G + a.tile_rows - 1) / a.tile_rows;
 }
 
-// Slice, request and tile of it that item of the batch is; false past the last. A request's last tile, which has the most
-// keys, comes first. Up to 64 requests stand in the lanes of every wave alike. Where they are mostly new (a.level_bits),
-// the last tiles of all requests come first, then the last but one of all, and so on, so that the longest start first:
-// with S(L) the sum of min(tiles, L), t is on level L with S(L) <= t < S(L + 1) (8 prompts of 1024 to 2048 tokens, 12
-// heads x 64: 98 -> 92 us). Else one request after another, whose tiles then share its keys in the L2 (8 chunks of 512
-// after 4096 to 8192 tokens, 32 heads x 128: 514 us, by levels 570), all slices of the tiles of more than 32 rows before
-// those of the quicker ones of few (40 requests that decode and 8 chunks: 113 -> 104 us).
+// Slice, request and tile of it that item of the batch is; false past the last. Up to 64 requests stand in the lanes of
+// every wave alike. Tiles of more than 32 rows come before those of few (with 128-row tiles; 40 requests that decode and 8
+// chunks: 113 -> 104 us), and those with the most keys first, by levels: on level L a request has the tile that ends L
+// tiles before the longest request's end, so that its tiles stand on levels off .. off + tiles - 1 and with S(L) the sum
+// of clamp(L - off, 0, tiles) place t is on the level with S(L) <= t < S(L + 1). The tiles
+// of a request still stand together where histories are long, and share its keys in the L2. (8 prompts of 1024 to 2048
+// tokens, 12 heads x 64: 98 us request by request, 87 so; 8 chunks of 512 after 4096 to 8192, 32 heads x 128: 529 and
+// 485, and 570 with levels from each request's own end.)
 __device__ __forceinline__ bool find_tile_64(const PagedPrefillArgs& a, int item, int& slice, int& b, int& own) {
   const int lane = threadIdx.x & 63;
   int first;
-  const int rows = lane < a.B ? tokens_of(a, lane, first) * a.G : 0, mine = (rows + a.tile_rows - 1) / a.tile_rows;
-  if (!a.level_bits) {
-    const int few = mine > 0 && rows - (mine - 1) * a.tile_rows <= kFewRows && a.tile_rows > kFewRows, many = mine - few;
-    unsigned incl = (unsigned)many;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned y = __shfl_up(incl, o, 64);
-      if (lane >= o) incl = add_many(incl, y);
-    }
-    const int most = min(__builtin_amdgcn_readlane((int)incl, 63), a.tiles);  // of ascending row starts: all
-    if (item < most * a.nsplit) {
-      slice = item / most;
-      const unsigned t = (unsigned)(item - slice * most), before = incl - (unsigned)many;
-      const unsigned long long it = __ballot(t >= before && t < incl && many > 0);
-      if (!it) return false;
-      b = (int)__ffsll((long long)it) - 1;
-      own = __builtin_amdgcn_readfirstlane(__shfl(many - 1 - (int)(t - before), b, 64));
-      return own >= 0;
-    }
-    const unsigned long long have = __ballot(few);
-    const int rest = item - most * a.nsplit, number = (int)__popcll(have);
-    if (!number) return false;
-    slice = rest / number;
-    const int rank = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(have >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)have, 0));
-    const unsigned long long it = __ballot(few && rank == rest - slice * number);
-    if (slice >= a.nsplit || !it) return false;
+  const int rows = lane < a.B ? tokens_of(a, lane, first) * a.G : 0, all = (rows + a.tile_rows - 1) / a.tile_rows;
+  const bool few = all > 0 && a.tile_rows > kFewRows && rows - (all - 1) * a.tile_rows <= kFewRows;
+  const int mine = all - few, most = min(wave_total(mine), a.tiles);  // of ascending row starts: all of them
+  const unsigned long long behind = ((unsigned long long)1 << lane) - 1;  // the lanes before this one
+  if (item < most * a.nsplit) {
+    slice = item / most;
+    const int t = item - slice * most, len = mine > 0 ? min(max(a.lengths[lane], 0), a.max_len) : 0;
+    const int off = (wave_most(len) - len) / max(1, a.tile_rows / a.G), end = mine > 0 ? off + mine : 0;
+    auto sum = [&](int level) __attribute__((always_inline)) { return wave_total(min(max(level - off, 0), mine)); };
+    int level = 0;  // the largest with S(level) <= t
+    for (int bit = 1 << (31 - __builtin_clz(wave_most(end) | 1)); bit; bit >>= 1)
+      if (sum(level + bit) <= t) level += bit;
+    const int rank = t - sum(level);
+    const bool has = level >= off && level < end;
+    const unsigned long long have = __ballot(has), it = __ballot(has && (int)__popcll(have & behind) == rank);
+    if (!it) return false;
     b = __builtin_amdgcn_readfirstlane((int)__ffsll((long long)it) - 1);
-    own = __builtin_amdgcn_readfirstlane(__shfl(many, b, 64));
+    own = __builtin_amdgcn_readlane(mine - 1 - (level - off), b);
     return true;
   }
-  slice = item / a.tiles;
-  const int t = item - slice * a.tiles;
-  auto sum = [&](int level) __attribute__((always_inline)) { return wave_total(min(mine, level)); };
-  int level = 0;  // the largest with S(level) <= t
-  for (int bit = a.level_bits; bit; bit >>= 1)
-    if (sum(level + bit) <= t) level += bit;
-  const unsigned long long have = __ballot(mine > level);
-  const int j = t - sum(level);
-  if (j < 0 || j >= (int)__popcll(have)) return false;
-  const int rank = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(have >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)have, 0));
-  const unsigned long long it = __ballot(mine > level && rank == j);
+  const unsigned long long have = __ballot(few);
+  const int rest = item - most * a.nsplit, number = (int)__popcll(have);
+  if (!number) return false;
+  slice = rest / number;
+  const unsigned long long it = __ballot(few && (int)__popcll(have & behind) == rest - slice * number);
+  if (slice >= a.nsplit || !it) return false;
   b = __builtin_amdgcn_readfirstlane((int)__ffsll((long long)it) - 1);
-  own = __builtin_amdgcn_readfirstlane(__shfl(mine, b, 64)) - 1 - level;
+  own = __builtin_amdgcn_readlane(mine, b);
   return true;
 }
 // More requests: one after another, by a scan of all threads. place has two ints.
@@ -695,10 +691,6 @@ template <class P, int D>
 hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
   a.tiles = (int)((int64_t)a.N * a.G / a.tile_rows + a.B);  // each request has one that is not whole
   a.map = make_tilemap(a.c.H, a.tiles * a.nsplit);
-  a.level_bits = 0;
-  if (a.B <= 64 && (int64_t)a.max_len * a.B <= 2 * (int64_t)a.N)
-    for (a.level_bits = 1; 2 * a.level_bits <= a.tiles; a.level_bits *= 2) {
-    }
   hipLaunchKernelGGL((prefill_kernel<P, D>), dim3((unsigned)grid_size(a.map)), dim3(kNT), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
@@ -713,7 +705,7 @@ hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
 
 // Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
 // * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short: one prompt of 2048
-//   tokens, 8 heads x 64, 29 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 98
+//   tokens, 8 heads x 64, 28 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 93
 //   against 327. With longer histories the keys that every tile reads again cost more than slices of 128-row tiles: a
 //   chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
 // * As many slices as bring the workgroups to what the chip holds at once (three a CU for bf16 of up to 64 channels,

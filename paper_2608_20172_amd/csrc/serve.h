@@ -93,7 +93,6 @@ struct PagedPrefillArgs {
   int tile_rows;             // rows of a tile
   int nsplit, slice;         // slices of `slice` keys
   int tiles;                 // at most so many tiles (set by the launch)
-  int level_bits;            // tiles by levels: a power of two over half of their number; else 0 (set by the launch)
   TileMap map;               // key heads x tiles x slices (set by the launch)
 };
 // The largest batch: every workgroup finds its tile by a scan over the requests.
