@@ -17,7 +17,7 @@
 // * Where the tiles leave CUs idle the histories are split into slices whose terminal
 //   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
-//   workgroup finds its tile by a scan over the requests' tile counts in LDS.
+//   workgroup finds its tile from the tile counts of all.
 // * A tile of 64 keys is gathered: each lane looks up the page of the key row that
 //   it loads, one tile ahead, and its 16-byte loads write LDS directly. Rows past
 //   the tile's last position are that position's again (masked), so nothing past a
@@ -87,8 +87,8 @@ __device__ __forceinline__ int tiles_of(const PagedPrefillArgs& a, int b) {
 // tiles before the longest request's end, so that its tiles stand on levels off .. off + tiles - 1 and with S(L) the sum
 // of clamp(L - off, 0, tiles) place t is on the level with S(L) <= t < S(L + 1). The tiles
 // of a request still stand together where histories are long, and share its keys in the L2. (8 prompts of 1024 to 2048
-// tokens, 12 heads x 64: 98 us request by request, 87 so; 8 chunks of 512 after 4096 to 8192, 32 heads x 128: 529 and
-// 485, and 570 with levels from each request's own end.)
+// tokens, 12 heads x 64: 98 us request by request, 87 so; 8 chunks of 256 to 512 after 4096 to 8192, 32 heads x 128:
+// 529 and 485, and 570 with levels from each request's own end.)
 __device__ __forceinline__ bool find_tile_64(const PagedPrefillArgs& a, int item, int& slice, int& b, int& own) {
   const int lane = threadIdx.x & 63;
   int first;
