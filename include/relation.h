@@ -547,7 +547,9 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  *   table      int32 [B, table_width]; lengths int32 [B], this step's tokens
  *              included; row_start int32 [B + 1], ascending, at most N
  *   row_stat   fp32 [N, Hq], optional: M_i = ln Z_i + lambda ln i
- *   workspace  relation_paged_prefill_workspace_bytes(c, d) bytes, 16-byte aligned
+ *   workspace  relation_paged_prefill_workspace_bytes(c, d) bytes, 16-byte aligned.
+ *              Fewer tokens may need more (their histories are split further): what
+ *              calls of several sizes share is the largest of theirs
  * max_length as in rel_paged_query. A request whose length is under n_b or over
  * that bound gets NaN rows, and so does a row if a page of its entries is not in the
  * pool. Entries past a request's length are not read; NaN and infinities in the
@@ -621,7 +623,8 @@ rel_status relation_sample(const rel_sample* s, const void* logits, const float*
  *              nobody: its output rows are 0, and so are its gradients.
  *   D <= 128; rope_dim even, 0 (no rotation) .. D; rope_base > 1.
  * At most 2^26 tokens and 2^16 heads. Angles are formed in 64 bits, sums in 32; each output is rounded once. NaN and
- * infinities stay in their row (in the backward pass also in the weights' gradients). */
+ * infinities stay in their row (in the backward pass also in the weights' gradients); a
+ * finite row whose sum of squares passes fp32 becomes 0. */
 typedef enum rel_rope_layout {
   REL_ROPE_HALF = 0,
   REL_ROPE_INTERLEAVED = 1

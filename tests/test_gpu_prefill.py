@@ -384,3 +384,36 @@ def test_prefill_head_dim_and_shapes_are_checked():
             _run({**s, **bad})
     with pytest.raises(ValueError, match="GPU"):
         R.relation_paged_prefill(s["q"].cpu(), s["kc"], s["vc"], _i32(s["table"]), _i32(s["lens"]), _i32(s["start"]), 0.4)
+
+
+@pytest.mark.parametrize("B,G,H,long", [(64, 4, 2, 40), (65, 4, 2, 40), (64, 1, 1, 900), (63, 9, 1, 5), (33, 2, 2, 3000), (7, 1, 3, 4500),
+                                        (64, 16, 8, 300)])
+def test_prefill_every_tile_is_somebodys(B, G, H, long):
+    """Requests of none, one, a tile's and many tokens behind histories of all lengths, in a shuffled order: every row is
+    written, and by the right workgroup."""
+    rng = np.random.default_rng(B + G + long)
+    added = rng.choice([0, 1, 1, 1, 8, 32 // G, 33, 128 // G, 128 // G + 1, 200], B)
+    chunks = [(int(c), int(n)) for c, n in zip(rng.integers(0, long, B), added)]
+    log(f"[prefill] {B} requests, {sum(added)} tokens after up to {long}")
+    s = _step(chunks, H, G, 32, 16, "bf16")
+    out = {"o": torch.full_like(s["q"], math.inf), "row_stat": torch.full((s["q"].shape[0], H * G), math.inf, device=DEV)}
+    r = _run(s, out=out)
+    assert torch.isfinite(r["o"]).all() and torch.isfinite(r["row_stat"]).all()
+    _close(r, s, "bf16", most=B)
+
+
+@pytest.mark.parametrize("chunks", [[(100, 60), (0, 40)], [(90, 3), (0, 5)], [(5000, 30)]])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_prefill_a_query_that_is_not_finite_spoils_its_row_alone(chunks, value):
+    s = _step(chunks, 2, 2, 64, 16, "bf16")
+    base = _run(s)
+    t = {**s, "q": s["q"].clone()}
+    t["q"][1, 3, 7] = value
+    r = _run(t)
+    assert not torch.isfinite(r["o"][1, 3]).any() or value == math.inf  # infinite evidence of either sign may leave a row
+    o, w = r["o"].clone(), base["o"].clone()
+    o[1, 3], w[1, 3] = 0, 0
+    assert rel_l2(_np(o), _np(w)) <= BAR["bf16"] and torch.equal(o[:, :2], w[:, :2])
+    m, n = r["row_stat"].clone(), base["row_stat"].clone()
+    m[1, 3] = n[1, 3] = 0
+    assert rel_l2(_np(m), _np(n)) <= BAR_M

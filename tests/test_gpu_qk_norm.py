@@ -337,3 +337,19 @@ def test_outputs_of_the_differentiable_call_are_its_own():
     q = torch.randn((5, 2, 16), device=DEV)
     with pytest.raises(ValueError, match="out"):
         R.relation_qk_norm(q, None, out={"q": torch.empty_like(q)})
+
+
+def test_rows_of_zeros_and_of_sums_past_32_bits():
+    """Zeros stay zeros, forward and back; where the sum of squares passes fp32 the row becomes 0, its neighbours stay."""
+    x = torch.randn((4, 2, 64), device=DEV)
+    want = R.relation_qk_norm_fwd(x, None)["q"]
+    y = x.clone()
+    y[1, 0], y[2, 1] = 0.0, 1.0e25
+    o = R.relation_qk_norm_fwd(y, None)["q"]
+    assert not o[1, 0].any() and not o[2, 1].any()
+    keep = torch.ones((4, 2), dtype=torch.bool, device=DEV)
+    keep[1, 0] = keep[2, 1] = False
+    assert torch.equal(o[keep], want[keep])
+    leaf = y.clone().requires_grad_()
+    R.relation_qk_norm(leaf, None)[0].sum().backward()
+    assert torch.isfinite(leaf.grad).all() and leaf.grad[1, 0].any()  # 1 / sqrt(eps) times the turned ones
