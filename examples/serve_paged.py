@@ -121,6 +121,8 @@ def new_rows(model, pool, m, x, one_each, longest):
 
 def take_in(model, pool, prompts, longest, chunk=None):
     """The prompts, up to `chunk` tokens of each a step: the hidden rows [T, dim] of each."""
+    if chunk is not None and chunk < 1:
+        raise ValueError("a chunk has at least one token")
     rows, at = [[] for _ in prompts], 0
     while at < max(len(p) for p in prompts):
         part = [p[at:at + (chunk or longest)] for p in prompts]

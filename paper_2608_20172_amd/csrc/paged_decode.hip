@@ -77,6 +77,58 @@ int64_t groups_launched(const PagedDecodeArgs& a) {
   return a.placed ? (groups + kDies - 1) / kDies * kDies : groups;
 }
 
+// The Self entry's reads of one wave: lane holds channels lane and lane + 64.
+struct SelfEntry {
+  float dot, v0, v1;  // q . k over the lane's channels; the own value
+  bool ok;
+};
+template <typename TI>
+__device__ __forceinline__ SelfEntry read_self(const PagedDecodeArgs& a, int b, int hq, int len, int lane) {
+  SelfEntry s{0.0f, 0.0f, 0.0f, false};
+  if (len < 1) return s;
+  int64_t off;
+  s.ok = entry_offset(a, b, hq / a.G, len - 1, off);
+  if (!s.ok) return s;
+  const TI* q = (const TI*)a.q + ((int64_t)b * a.Hq + hq) * a.c.D;
+  const TI *k = (const TI*)a.k + off, *v = (const TI*)a.v + off;
+  if (lane < a.c.D) {
+    s.dot = Elem<TI>::load(q + lane) * Elem<TI>::load(k + lane);
+    s.v0 = Elem<TI>::load(v + lane);
+  }
+  if (lane + 64 < a.c.D) {
+    s.dot += Elem<TI>::load(q + lane + 64) * Elem<TI>::load(k + lane + 64);
+    s.v1 = Elem<TI>::load(v + lane + 64);
+  }
+  return s;
+}
+
+// Eqs. 12-13 of one row by one wave: state (m, l) with z0, z1 at channels lane, lane + 64.
+template <typename TI>
+__device__ __forceinline__ void finish_row(const PagedDecodeArgs& a, int b, int hq, int len, int lane, SelfEntry s,
+                                           float m, float l, float z0, float z1) {
+  float d = s.dot;
+  for (int o = 32; o >= 1; o >>= 1) d += __shfl_xor(d, o, 64);
+  const float S = 1.0f / (1.0f + expf(-d * a.scale * a.inv_tau));
+  const float ln_i = logf((float)len);
+  const float lam = *a.lambda;
+  float g = 0.0f, omg = 1.0f, zr0 = 0.0f, zr1 = 0.0f, lnZ = S;
+  if (!(l == 0.0f)) {                               // some history (or a NaN in it)
+    const float A = m * kLn2 + logf(l) - lam * ln_i;       // A_i = L^E_i - lambda ln i (eq. 5)
+    g = 1.0f / (1.0f + expf(S - A));                // g = sigmoid(A - S)
+    omg = 1.0f / (1.0f + expf(A - S));              // 1 - g = sigmoid(S - A)
+    const float il = 1.0f / l;
+    zr0 = z0 * il;
+    zr1 = z1 * il;
+    lnZ = fmaxf(S, A) + log1pf(expf(-fabsf(S - A)));
+  }
+  // a length outside 1 .. max_len or a page outside the pool: NaN, so that the error is seen
+  const float nan = __builtin_nanf("");
+  TI* o = (TI*)a.out + ((int64_t)b * a.Hq + hq) * a.c.D;
+  if (lane < a.c.D) Elem<TI>::store(o + lane, s.ok ? omg * s.v0 + g * zr0 : nan);
+  if (lane + 64 < a.c.D) Elem<TI>::store(o + lane + 64, s.ok ? omg * s.v1 + g * zr1 : nan);
+  if (lane == 0 && a.row_stat) a.row_stat[(int64_t)b * a.Hq + hq] = s.ok ? lnZ + lam * ln_i : nan;
+}
+
 // Offsets (of head h) of the pages of slice [s0, s0 + slice) into LDS, by all NT
 // threads, and whether the thread met a bad page that holds keys of the request's
 // history. The table is read before the length is looked at: the two reads run side
@@ -110,7 +162,7 @@ __device__ __forceinline__ void join_waves(const PagedDecodeArgs& a, int slice, 
     merge_into<2>(m, l, z, s[0], s[1], zo);
   }
   if (a.nsplit == 1) {
-    finish_row<TI>(a, (int64_t)b * a.Hq + hq, len, lane, self, m, l, z[0], z[1]);
+    finish_row<TI>(a, b, hq, len, lane, self, m, l, z[0], z[1]);
     return;
   }
   float* out = a.states + ((int64_t)slice * a.B * a.Hq + (int64_t)b * a.Hq + hq) * (D + 2);
@@ -154,7 +206,7 @@ __global__ __launch_bounds__(kStatesT) void paged_states_f32_kernel(PagedDecodeA
   const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
   int bad = page_offsets<NT>(a, b, h, s0, len, offs);
   SelfEntry self{};
-  if (a.nsplit == 1 && w < ng) self = read_self<TI>(a, b, (int64_t)b * a.Hq + hq0 + w, hq0 + w, len, lane);
+  if (a.nsplit == 1 && w < ng) self = read_self<TI>(a, b, hq0 + w, len, lane);
   if (s1 <= s0 && a.nsplit > 1) return;  // a slice past the request's end: nobody reads its state
 
   float m[GQ], l[GQ], z[GQ][VEC];
@@ -307,7 +359,7 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
   const int mask = (1 << a.c.shift) - 1, p0 = s0 >> a.c.shift;
   int bad = page_offsets<NW * 64>(a, b, h, s0, len, offs);
   SelfEntry self{};
-  if (a.nsplit == 1 && w < ng) self = read_self<bf16>(a, b, (int64_t)b * a.Hq + hq0 + w, hq0 + w, len, lane);
+  if (a.nsplit == 1 && w < ng) self = read_self<bf16>(a, b, hq0 + w, len, lane);
   if (s1 <= s0 && a.nsplit > 1) return;   // a slice past the request's end: nobody reads its state
 
   float m = kNegInf, l = 0.0f;
@@ -442,7 +494,7 @@ __global__ __launch_bounds__(NW * 64) void paged_states_bf16_kernel(PagedDecodeA
   }
   __syncthreads();
   for (int y = w; y < ng; y += NW) {
-    if (a.nsplit == 1 && y >= NW) self = read_self<bf16>(a, b, (int64_t)b * a.Hq + hq0 + y, hq0 + y, len, lane);
+    if (a.nsplit == 1 && y >= NW) self = read_self<bf16>(a, b, hq0 + y, len, lane);
     join_waves<bf16, NW>(a, slice, b, hq0 + y, len, lane, reinterpret_cast<const float*>(vlds[0]) + y * SW, WAVEB / 4,
                          self);
   }
@@ -467,7 +519,7 @@ __global__ __launch_bounds__(kMergeT) void paged_merge_kernel(PagedDecodeArgs a)
   const int64_t stride_s = (int64_t)a.B * a.Hq * (D + 2);
   const float* st0 = a.states + (int64_t)n * (D + 2);
   SelfEntry self{};
-  if (w == 0) self = read_self<TI>(a, b, n, hq, len, lane);  // first, so that it overlaps the states' reads
+  if (w == 0) self = read_self<TI>(a, b, hq, len, lane);  // first, so that it overlaps the states' reads
   const int grp = tid / G, c0 = 2 * (tid % G);
   const int cz = c0 < D ? c0 : 0;  // lanes past the width repeat the first pair; nobody reads theirs
   float m = kNegInf, l = 0.0f, z[2] = {0.0f, 0.0f};
@@ -499,7 +551,7 @@ __global__ __launch_bounds__(kMergeT) void paged_merge_kernel(PagedDecodeArgs a)
     const float zo[2] = {zsh[x][lane], G > 32 ? zsh[x][(64 + lane) % (2 * G)] : 0.0f};
     merge_into<2>(m, l, z, mls[x][0], mls[x][1], zo);
   }
-  finish_row<TI>(a, n, len, lane, self, m, l, z[0], z[1]);
+  finish_row<TI>(a, b, hq, len, lane, self, m, l, z[0], z[1]);
 }
 
 // Bytes of LDS for the offsets of a slice's pages.

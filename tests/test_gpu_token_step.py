@@ -221,6 +221,13 @@ def test_example_with_chunks_and_norms(chunk, head_norm, width):
     assert [len(a) for a, _ in scores] == [len(p) - 1 for p in prompts]
 
 
+def test_example_chunks_have_tokens():
+    model = E.Decoder(vocab=301, layers=1, heads=2, width=32)
+    for chunk in (0, -1):
+        with pytest.raises(ValueError, match="chunk"):
+            E.generate(model, _prompts(model, (3,)), 1, chunk=chunk)
+
+
 def test_example_scores_are_the_prompts_own():
     """Log-probabilities to 1e-5 and ranks by the definition from the same logits."""
     model = E.Decoder(vocab=3001, layers=2, heads=4, width=64, head_norm=True)
