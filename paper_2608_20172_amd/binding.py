@@ -1216,6 +1216,22 @@ def relation(q, k, v, lam, tau_s: float = TAU_S, scale: Optional[float] = None) 
     return _RelationFn.apply(q, k, v, lam, tau_s, scale)
 
 
+def _capturable(*outs):
+    """The outputs of a differentiable call, unless it is captured and a graph of earlier eager calls on one of its leaves
+    still lives: a captured backward pass would then wait for the eager stream that the leaf's gradient sum is tied to,
+    and torch ends the process. The first eager call leaves its stream at the node that all graphs of a leaf share."""
+    fn = next((o.grad_fn for o in outs if o is not None and o.grad_fn is not None), None)
+    for node, _ in () if fn is None else fn.next_functions:
+        if node is not None and node.name() == "torch::autograd::AccumulateGrad":
+            stream = torch.cuda.current_stream(node.variable.device).cuda_stream
+            if not torch.cuda.is_current_stream_capturing():
+                node.metadata.setdefault("relation_stream", stream)
+            elif node.metadata.get("relation_stream", stream) != stream:
+                raise RuntimeError("captured while an eager graph of the same leaf lives on another stream: let it go "
+                                   "first, or capture under torch.no_grad() what has no backward pass")
+    return outs
+
+
 class _QkNormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, positions, opts):
@@ -1235,10 +1251,10 @@ class _QkNormFn(torch.autograd.Function):
 
 def relation_qk_norm(q, k, q_weight=None, k_weight=None, positions=None, **opts):
     """Differentiable relation_qk_norm_fwd (its options but ``out``): (q, k) normed and rotated, gradients for q, k and the
-    weights. To capture the backward pass into a graph, let no graph of earlier eager calls on the same leaves live."""
+    weights. It is not captured into a graph while a graph of earlier eager calls on the same leaves lives."""
     if "out" in opts:
         raise ValueError("out: outputs of their own only")
-    return _QkNormFn.apply(q, k, q_weight, k_weight, positions, opts)
+    return _capturable(*_QkNormFn.apply(q, k, q_weight, k_weight, positions, opts))
 
 
 class _TokenLogprobsFn(torch.autograd.Function):
@@ -1259,6 +1275,6 @@ class _TokenLogprobsFn(torch.autograd.Function):
 
 
 def relation_token_logprobs(logits, tokens):
-    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]. To
-    capture the backward pass into a graph, let no graph of earlier eager calls on the same leaves live."""
-    return _TokenLogprobsFn.apply(logits, tokens)
+    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]. It
+    is not captured into a graph while a graph of earlier eager calls on the same leaf lives."""
+    return _capturable(*_TokenLogprobsFn.apply(logits, tokens))

@@ -137,6 +137,56 @@ def test_training_step_in_32_bits():
         assert abs(got - diff) <= 1e-3 * size, (got, diff)
 
 
+def test_captured_training_step():
+    """Norms, Relation and log-probabilities with their backward passes in a graph: the eager gradients' bits on every
+    replay; refused while an eager graph of the same leaves lives."""
+    rng = np.random.default_rng(30)
+    B, H, T, D = 2, 2, 100, 64
+    mk = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(torch.bfloat16).to(DEV)
+    q, k, wq, z = mk(B, H, T, D), mk(B, H, T, D), mk(D).float(), mk(60, 500)
+    tokens = torch.from_numpy(rng.integers(-1, 500, 60)).to(DEV)
+    leaves = [t.requires_grad_() for t in (q, k, wq, z)]
+    v, lam, c = mk(B, H, T, D), torch.full((), 0.3, device=DEV), mk(B, H, T, D)
+
+    def loss():
+        a, b = R.relation_qk_norm(q, k, wq, None)
+        lp, ent = R.relation_token_logprobs(z, tokens)
+        return (R.relation(a, b, v, lam) * c).float().sum() + (lp * 0.5).sum() + (ent * 0.1).sum()
+
+    def step():
+        return torch.autograd.grad(loss(), leaves)
+    live = loss()
+    for call in (lambda: R.relation_qk_norm(q, k, wq, None), lambda: R.relation_token_logprobs(z, tokens)):
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="lives"):
+            with torch.cuda.graph(graph):
+                call()
+        with torch.no_grad():  # nothing to differentiate, nothing to refuse
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                call()
+    del live
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for turn in range(4):
+        with torch.no_grad():
+            for t in leaves:
+                t.mul_(1.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        held = [t.clone() for t in got]
+        want = step()
+        torch.cuda.synchronize()
+        for x, y in zip(held, want):
+            assert torch.equal(x, y), turn
+
+
 def test_captured_steps_that_share_their_workspaces():
     """Two graphs of a step over the same caches and workspaces, replayed in turn with eager work between: the eager
     step's bits."""
