@@ -10,10 +10,10 @@
 //   that a key head that they share is read once for all. A lane's row has a
 //   position of its own, anywhere in its 32-key block.
 // * A tile of at most 32 rows (a decoding request among chunks, a short chunk) gives
-//   each wave 32 of every 128 keys instead; the four partial sums meet in LDS. With
-//   the reference at 0 they only add. (40 requests that decode and 8 chunks of 128 to
+//   each wave 32 of every 128 keys instead, which it loads for itself; the four
+//   partial sums meet in LDS. With the reference at 0 they only add. (40 requests that decode and 8 chunks of 128 to
 //   256 tokens over 410 to 4096 keys, 16 heads of width 128 on 4: 194 us with such a
-//   tile's rows all on one wave, now 118.)
+//   tile's rows all on one wave, 119 with barriers around the loads, now 109.)
 // * Where the tiles leave CUs idle the histories are split into slices whose terminal
 //   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
@@ -29,7 +29,7 @@
 // What bounds it is the vector work of a weight, about 9 instructions a lane and
 // entry beside one matrix instruction, as in the fused forward pass, and the waits
 // of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
-// 690 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 76 us. On
+// 690 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
 // the same rows in one dense tensor the fused forward pass, which looks nothing up,
 // takes 62 us against 73 (8 x 12 x 1536 x 64) and 163 against 199 (4 x 8 x 4096 x 128).
 #include "kernels.h"
@@ -516,26 +516,32 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
     load_tile<P>(a, k, v, kt, w, lane, jlast, id, Kd, Vd, bad);
     look_up<P>(a, trow, kt + 1, w, lane, jlast, id);  // past the last tile: the last key's page again
   };
-  look_up<P>(a, trow, kt0, w, lane, jlast, id);
   if (few) {
-    // 128 keys at a time: waves 0, 1 the blocks of the first tile, waves 2, 3 those of the second
-    for (int kt = kt0; kt < nkt; kt += 2) {
-      if (kt > kt0) __syncthreads();  // the tiles before are read
-      load(kt, KA, VA);
-      load(kt + 1, KB, VB);
+    // 128 keys at a time: waves 0, 1 the blocks of the first tile, waves 2, 3 those of the second. A wave loads what it
+    // reads, and waits for nobody.
+    const int krow = 32 * (w & 1), part = 2 * (w & 1);
+    unsigned char* Ks = w >> 1 ? KB : KA;
+    unsigned char* Vs = w >> 1 ? VB : VA;
+    int kt = kt0 + (w >> 1), id2[Gather<P>::ROWS];
+    look_up<P>(a, trow, kt, part, lane, jlast, id);
+    look_up<P>(a, trow, kt, part + 1, lane, jlast, id2);
+    for (; kt * kBK + krow <= jlast && kt < nkt; kt += 2) {
+      load_tile<P>(a, k, v, kt, part, lane, jlast, id, Ks, Vs, bad);
+      load_tile<P>(a, k, v, kt, part + 1, lane, jlast, id2, Ks, Vs, bad);
+      look_up<P>(a, trow, kt + 2, part, lane, jlast, id);
+      look_up<P>(a, trow, kt + 2, part + 1, lane, jlast, id2);
       wait_loads();
-      __syncthreads();
-      const int k0 = (kt + (w >> 1)) * kBK + 32 * (w & 1), krow = 32 * (w & 1);
-      const unsigned char* Ks = w >> 1 ? KB : KA;
-      const unsigned char* Vs = w >> 1 ? VB : VA;
-      Op pop[2] = {Op{}, Op{}};
-      if (k0 <= jlast) {
-        const floatx16 s = evidence<P, KS>(Ks, krow, qop, L);
-        fast_block<P, D, QM, true>(s, m, l, uii, pop, L, me.pos - k0, c);
-      }
+      asm volatile("" ::: "memory");  // no read of them before
+      Op pop[2];
+      const floatx16 s = evidence<P, KS>(Ks, krow, qop, L);
+      fast_block<P, D, QM, true>(s, m, l, uii, pop, L, me.pos - kt * kBK - krow, c);
       add_values<P, D>(Vs, krow, 0, pop, oacc, L);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads from LDS have ended
     }
+    __syncthreads();  // bad_key is set
   } else {
+    look_up<P>(a, trow, kt0, w, lane, jlast, id);
     const int phi = wrow < t.rows ? position_of(a, t, wrow + 31) : -1;  // the wave's last position
     auto fast_step = [&](auto full, int kt, const unsigned char* Ks, const unsigned char* Vs, unsigned char* Kn,
                          unsigned char* Vn) __attribute__((always_inline)) {
@@ -705,7 +711,7 @@ hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
 
 // Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
 // * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short: one prompt of 2048
-//   tokens, 8 heads x 64, 28 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 93
+//   tokens, 8 heads x 64, 26 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 88
 //   against 327. With longer histories the keys that every tile reads again cost more than slices of 128-row tiles: a
 //   chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
 // * As many slices as bring the workgroups to what the chip holds at once (three a CU for bf16 of up to 64 channels,
