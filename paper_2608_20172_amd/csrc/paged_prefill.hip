@@ -11,9 +11,10 @@
 //   position of its own, anywhere in its 32-key block.
 // * A tile of at most 32 rows (a decoding request among chunks, a short chunk) gives
 //   each wave 32 of every 128 keys instead, which it loads for itself; the four
-//   partial sums meet in LDS. With the reference at 0 they only add. (40 requests that decode and 8 chunks of 128 to
-//   256 tokens over 410 to 4096 keys, 16 heads of width 128 on 4: 194 us with such a
-//   tile's rows all on one wave, 119 with barriers around the loads, now 109.)
+//   partial sums meet in LDS. With the reference at 0 they only add. (40 requests
+//   that decode and 8 chunks of 128 to 256 tokens over 410 to 4096 keys, 16 heads of
+//   width 128 on 4: 194 us with such a tile's rows all on one wave, 119 with barriers
+//   around the loads, now 110.)
 // * Where the tiles leave CUs idle the histories are split into slices whose terminal
 //   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
@@ -29,9 +30,9 @@
 // What bounds it is the vector work of a weight, about 9 instructions a lane and
 // entry beside one matrix instruction, as in the fused forward pass, and the waits
 // of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
-// 690 us (0.8 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
+// 665 us (0.85 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
 // the same rows in one dense tensor the fused forward pass, which looks nothing up,
-// takes 62 us against 73 (8 x 12 x 1536 x 64) and 163 against 199 (4 x 8 x 4096 x 128).
+// takes 62 us against 71 (8 x 12 x 1536 x 64) and 167 against 194 (4 x 8 x 4096 x 128).
 #include "kernels.h"
 #include "lanes.h"
 #include "paged_row.h"
@@ -710,10 +711,12 @@ hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
 }  // namespace
 
 // Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
-// * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short: one prompt of 2048
-//   tokens, 8 heads x 64, 26 us against 42; five chunks of 151 to 301 tokens after up to 777, 8 heads x 80 in fp32, 88
-//   against 327. With longer histories the keys that every tile reads again cost more than slices of 128-row tiles: a
-//   chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
+// * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short, and, where requests
+//   have 64 rows and more, up to two tiles a CU of 64 channels, five for four CUs of more. One prompt of 2048 tokens, 8
+//   heads x 64, 26 us against 42, four 45 against 59 (416 tiles), two of 4096 68 against 87 (400); 8 heads x 128, one of
+//   4096 88 against 101 (264), but four of 2048 84 against 74 (416); five chunks of 151 to 301 tokens after up to 777, 8
+//   heads x 80 in fp32, 88 against 327. With longer histories the keys that every tile reads again cost more than
+//   slices of 128-row tiles: a chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
 // * As many slices as bring the workgroups to what the chip holds at once (three a CU for bf16 of up to 64 channels,
 //   else two), each of 512 keys or more: a chunk of 2048 after 32768, 16 heads on 4 x 128, 687 to 716 us in two slices,
 //   903 to 927 in one, 683 to 706 in four; 7 chunks of 128 to 256 after up to 4096 78 in four, 124 in one. Tiles of 32
@@ -723,7 +726,8 @@ PrefillPlan paged_prefill_plan(int64_t N, int64_t B, int64_t H, int64_t G, int64
   const int64_t kTarget = dtype == 1 && D <= 64 ? 768 : 512;  // what the chip holds at once
   PrefillPlan p;
   auto groups = [&](int64_t rows) { return (N * G / rows + B) * H; };
-  p.tile_rows = groups(kRows) <= 256 && max_len <= 4096 ? kFewRows : kRows;
+  const int64_t scarce = N * G < 64 * B ? 256 : D <= 64 ? 512 : 320;
+  p.tile_rows = groups(kRows) <= scarce && max_len <= 4096 ? kFewRows : kRows;
   const int64_t have = groups(p.tile_rows);
   int64_t split = p.tile_rows == kFewRows && have >= 256 ? 1 : (kTarget + have - 1) / have;
   const int64_t most = (max_len + kMinSlice - 1) / kMinSlice;

@@ -417,3 +417,12 @@ def test_prefill_a_query_that_is_not_finite_spoils_its_row_alone(chunks, value):
     m, n = r["row_stat"].clone(), base["row_stat"].clone()
     m[1, 3] = n[1, 3] = 0
     assert rel_l2(_np(m), _np(n)) <= BAR_M
+
+
+@pytest.mark.parametrize("B,H,D,n,dtype", [(3, 8, 64, 1500, "bf16"), (1, 8, 128, 3000, "bf16"), (40, 8, 64, 80, "bf16"), (3, 8, 80, 700, "f32"),
+                                           (33, 8, 64, 1, "bf16"), (5, 16, 32, 900, "bf16")])
+def test_prefill_sizes_between_few_and_many_tiles(B, H, D, n, dtype):
+    """Fresh and cached chunks where the rule for a tile's rows changes."""
+    chunks = [((b * 131) % 400, max(1, n - 17 * b)) for b in range(B)]
+    s = _step(chunks, H, 1, D, 16, dtype)
+    _close(_run(s), s, dtype, most=24)
