@@ -30,7 +30,7 @@
 // What bounds it is the vector work of a weight, about 9 instructions a lane and
 // entry beside one matrix instruction, as in the fused forward pass, and the waits
 // of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
-// 665 us (0.85 PFLOP/s), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
+// 665 to 693 us (0.82 PFLOP/s and more), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
 // the same rows in one dense tensor the fused forward pass, which looks nothing up,
 // takes 62 us against 71 (8 x 12 x 1536 x 64) and 167 against 194 (4 x 8 x 4096 x 128).
 #include "kernels.h"
