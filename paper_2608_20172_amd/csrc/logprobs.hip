@@ -426,19 +426,20 @@ __global__ __launch_bounds__(kT, TOP ? 6 : 1) void logprobs_kernel(LogprobArgs a
           listed += __popcll(who);
         }
       };
-      if (!few) {
-        if (__any(m > over)) {
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) list(p.x(s, e) > over, p.x(s, e), p.at(s) + e);
-        }
-      } else {
+      // Places left out are -kWild in a tame wave, -inf in others: under the bound, but where a mask of a finite value is
+      // the bound (-2^119 and less) or -inf may be listed.
+      if (few || (p.tame && over < -kWild)) {
+        const unsigned least = few ? cut : 0u;  // a tame wave's logits are all over such a bound
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
           for (int e = 0; e < VE; ++e)
-            list(p.real(s, e) && ordered(p.x(s, e) + 0.0f) >= cut, p.x(s, e), p.at(s) + e);
+            list(p.real(s, e) && ordered(p.x(s, e) + 0.0f) >= least, p.x(s, e), p.at(s) + e);
+      } else if (__any(m > over)) {
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) list(p.x(s, e) > over, p.x(s, e), p.at(s) + e);
       }
       if (lane == 0) sh.count[w] = listed;
       if (tid < held) sh.held[tid] = first[tid];

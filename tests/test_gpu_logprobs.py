@@ -335,3 +335,31 @@ def test_given_outputs_and_arguments():
         R.relation_token_logprobs_fwd(x, t, out={"logprob": torch.empty(5, device=DEV)})
     e = R.relation_token_logprobs_fwd(x[:0], t[:0], top=3)
     assert e["logprob"].shape == (0,) and R.relation_token_logprobs_bwd(x[:0], t[:0], e["stats"]).shape == (0, 100)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,left", [(260, 4), (261, 5), (263, 7), (300, 3), (515, 3), (516, 4), (517, 1), (772, 4), (2050, 2),
+                                    (4099, 3), (30725, 5), (61445, 5)])
+def test_rows_masked_everywhere_but_at_the_end(V, left, dtype):
+    """A mask of a finite value under -2^119 on all but the last logits: the alternatives past those are masked tokens, the
+    lowest indices first, each once."""
+    rng = np.random.default_rng(V)
+    lowest = float(torch.finfo(TORCH_DT[dtype]).min)
+    rows = np.stack([np.full(V, x) for x in (lowest, -1.0e38, lowest, -7.0e35, -6.0e35, -1.0e30)])
+    rows[:, V - left:] = rng.standard_normal((len(rows), left))
+    rows[2, 1] = 0.5  # one at the front as well
+    x = torch.from_numpy(rows).to(TORCH_DT[dtype]).to(DEV)
+    n = len(rows)
+    for top in (1, left, left + 1, 8, 20, 32):
+        _check(x, [V - 1] * n, top, grad=False)
+    _check(x, [0, V - left, 1, V - 2, 3, V // 2], 20)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 30725), ("f32", 31743), ("bf16", 61445), ("bf16", 63487)])
+def test_many_rows_masked_everywhere_but_at_the_end(V, dtype):
+    """The same in a workgroup's last of several sub-chunks, when all before it are masked."""
+    N, left = 600, V % 1024 if V % 1024 < 8 else 5
+    x = torch.full((N, V), float(torch.finfo(TORCH_DT[dtype]).min), dtype=TORCH_DT[dtype], device=DEV)
+    x[:, V - left:] = torch.from_numpy(np.random.default_rng(V).standard_normal((N, left))).to(x)
+    for top in (left, left + 1, 20, 32):
+        _check(x, [V - 1 - n % 3 for n in range(N)], top, grad=False, rows=[0, 1, 300, 599])
