@@ -144,7 +144,9 @@ __device__ __forceinline__ int keys_over(const Key* list, int n, Key mine) {
   return place;
 }
 // The K first of all lists into out, in order: an entry's place is the number of entries over it, counted by four lanes,
-// each over one wave's list.
+// each over one wave's list. Every place of the first min(K, n) gets its entry because no two keys are alike: a logit is
+// listed by the one thread whose piece it is (real()), in the sub-chunk that has it. Places from n on are left as they
+// were; the lists of a row have K entries in all, as K is at most V.
 __device__ __forceinline__ void first_keys(const Lists& l, int held, int K, Key* out) {
   const int sub = threadIdx.x & 3;
   int n = held, count[kNW];
