@@ -1125,10 +1125,10 @@ def relation_token_logprobs_fwd(logits, tokens, *, top: int = 0, want_rank: bool
     K = int(top)
     p = RelTokenLogprobs(N, V, K, _dtype_code(logits.dtype), sl, 0)
     f32, i32, i64, k = torch.float32, torch.int32, torch.int64, max(K, 0)
-    if out is None:  # one allocation for the fp32 outputs
-        stats, logprob, entropy, tl = logits.new_empty(N * (6 + k), dtype=f32).split_with_sizes((4 * N, N, N, k * N))
-        stats, tl, tt = stats.view(N, 4), tl.view(N, k), logits.new_empty((N, k), dtype=i64)
+    if out is None:  # tensors of their own: parts of one would share its version counter, and one kept would keep all
+        logprob, entropy, stats = logits.new_empty(N, dtype=f32), logits.new_empty(N, dtype=f32), logits.new_empty((N, 4), dtype=f32)
         rank = logits.new_empty(N, dtype=i32) if want_rank else None
+        tt, tl = logits.new_empty((N, k), dtype=i64), logits.new_empty((N, k), dtype=f32)
     else:
         def new(name, shape, dtype):
             t = _given(out, name, shape, dtype, dev)
