@@ -992,10 +992,10 @@ def _head_rows(t: torch.Tensor) -> torch.Tensor:
 
 def _dense_like(t: torch.Tensor) -> torch.Tensor:
     """A dense tensor of t's shape with its order of heads and tokens: heads side by side as in a projection's output, or
-    a head's tokens one after another."""
+    a head's tokens one after another. No view: views that a differentiable call returns refuse in-place work."""
     if t.dim() == 4 and t.stride(2) >= t.stride(1) and t.shape[1] > 1:
         B, H, T, D = t.shape
-        return t.new_empty((B, T, H, D)).transpose(1, 2)
+        return t.new_empty_strided((B, H, T, D), (T * H * D, D, H * D, 1))
     return t.new_empty(t.shape)
 
 

@@ -353,3 +353,25 @@ def test_rows_of_zeros_and_of_sums_past_32_bits():
     leaf = y.clone().requires_grad_()
     R.relation_qk_norm(leaf, None)[0].sum().backward()
     assert torch.isfinite(leaf.grad).all() and leaf.grad[1, 0].any()  # 1 / sqrt(eps) times the turned ones
+
+
+@pytest.mark.parametrize("place", ["heads first", "tokens first", "packed"])
+def test_outputs_are_worked_on_in_place(place):
+    """Scaled and masked in place by the caller: the gradients of the same in 64 bits by hand (bars as above)."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    shape = {"heads first": (2, 3, 5, 64), "tokens first": (2, 5, 3, 64), "packed": (10, 3, 64)}[place]
+    x = torch.randn(shape, device=DEV, generator=g)
+    q = (x.transpose(1, 2) if place == "tokens first" else x).requires_grad_()
+    k = q.detach().clone().requires_grad_()
+    a, b = R.relation_qk_norm(q, k)
+    scale = torch.tensor([0.5, 0.0, 2.0], device=DEV).view((1, 3, 1, 1) if a.dim() == 4 else (1, 3, 1))
+    a *= scale
+    a[..., :7] = 0.0
+    b.mul_(2.0)
+    b.masked_fill_(scale == 0, 0.0)
+    (a.sum() + (b * b.detach()).sum()).backward()
+    da, db = torch.ones_like(a) * scale, b.detach() * 2.0 * (scale != 0)
+    da[..., :7] = 0.0
+    for leaf, d in ((q, da), (k, db)):
+        want = R.relation_qk_norm_bwd(leaf.detach(), None, None, None, d, None)["dq"]
+        assert torch.equal(leaf.grad, want)
