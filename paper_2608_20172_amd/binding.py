@@ -1219,7 +1219,11 @@ def relation(q, k, v, lam, tau_s: float = TAU_S, scale: Optional[float] = None) 
 def _capturable(*outs):
     """The outputs of a differentiable call, unless it is captured and a graph of earlier eager calls on one of its leaves
     still lives: a captured backward pass would then wait for the eager stream that the leaf's gradient sum is tied to,
-    and torch ends the process. The first eager call leaves its stream at the node that all graphs of a leaf share."""
+    and torch ends the process. The first eager call leaves its stream at the node that all graphs of a leaf share.
+    torch tells nobody that node's own stream, so this sees the ordinary mistake only, a step captured while a loss of an
+    eager one is held: inputs of this call that are leaves, and eager use of them by these calls. Leaves behind other
+    operations (the weight of the product that makes the logits), and those that only other operations have used,
+    relation() among them, are the caller's to look after."""
     fn = next((o.grad_fn for o in outs if o is not None and o.grad_fn is not None), None)
     for node, _ in () if fn is None else fn.next_functions:
         if node is not None and node.name() == "torch::autograd::AccumulateGrad":
@@ -1251,7 +1255,9 @@ class _QkNormFn(torch.autograd.Function):
 
 def relation_qk_norm(q, k, q_weight=None, k_weight=None, positions=None, **opts):
     """Differentiable relation_qk_norm_fwd (its options but ``out``): (q, k) normed and rotated, gradients for q, k and the
-    weights. It is not captured into a graph while a graph of earlier eager calls on the same leaves lives."""
+    weights. A training step is captured when no eager graph of its leaves lives (no loss of an eager step is held): torch
+    ends the process else. Where an input is a leaf that such a call has used, this one refuses to be captured; a
+    forward pass alone is captured under torch.no_grad()."""
     if "out" in opts:
         raise ValueError("out: outputs of their own only")
     return _capturable(*_QkNormFn.apply(q, k, q_weight, k_weight, positions, opts))
@@ -1275,6 +1281,7 @@ class _TokenLogprobsFn(torch.autograd.Function):
 
 
 def relation_token_logprobs(logits, tokens):
-    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V]. It
-    is not captured into a graph while a graph of earlier eager calls on the same leaf lives."""
+    """Differentiable (logprob, entropy) of the tokens (int64 [N]; negative: none) under each row of logits [N, V].
+    Captured as relation_qk_norm is: while no eager graph of the step's leaves lives; logits that are a leaf which such a
+    call has used are refused, the leaves behind computed ones are not looked at."""
     return _capturable(*_TokenLogprobsFn.apply(logits, tokens))
