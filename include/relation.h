@@ -535,7 +535,7 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
                                  size_t workspace_bytes, void* stream);
 
 /* A chunk of new tokens of each request over pages: the rows that
- * relation_paged_decode would give one token at a time, for prompts (whole, in
+ * relation_paged_decode would give one token at a time (bf16 roundings: below), for prompts (whole, in
  * parts, or after a prefix that is in the cache already) and for steps where some
  * requests add one token and others many. Request b's n_b = row_start[b + 1] -
  * row_start[b] tokens stand in rows row_start[b] .. of q, as relation_page_map
@@ -554,7 +554,10 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  * that bound gets NaN rows, and so does a row if a page of its entries is not in the
  * pool. Entries past a request's length are not read; NaN and infinities in the
  * entries after a row do not reach it. An infinite value among a row's own entries
- * may come out as NaN in its channel. B at most 4096, B H at most 2^22, N at most 2^26, N Hq at most
+ * may come out as NaN in its channel. In bf16 the weights of the values have 16 significant bits,
+ * as relation_paged_decode's have, where a request has at most 32 rows of a key head
+ * (n_b Hq / H); in larger chunks they may be rounded to bf16 once, as relation_fwd's are
+ * (2^-8 of each at most). B at most 4096, B H at most 2^22, N at most 2^26, N Hq at most
  * 2^30. */
 typedef struct rel_paged_chunk {
   int64_t N, B, Hq, table_width, max_length;

@@ -14,7 +14,15 @@
 //   partial sums meet in LDS. With the reference at 0 they only add. (40 requests
 //   that decode and 8 chunks of 128 to 256 tokens over 410 to 4096 keys, 16 heads of
 //   width 128 on 4: 194 us with such a tile's rows all on one wave, 119 with barriers
-//   around the loads, now 110.)
+//   around the loads, 91 without.) Its bf16 weights go into the products with V in two
+//   parts, 16 significant bits, as the decode step's do, so that a request that decodes
+//   loses nothing by coming here: 93 us against those 91, and one prompt of 2048 tokens (8
+//   heads x 64, tiles of 32 rows) 27 against 25.
+// * In tiles of 128 rows the weights are rounded to bf16 once, as in the fused forward
+//   pass (each off by at most 2^-8 of itself, so y by 2^-8 of its weighted values): they
+//   are bound by vector work, and two parts would cost 85 us against 74 for 8 prompts of
+//   1024 to 2048 tokens, 12 heads x 64, and 868 against 672 for 2048 tokens after 32768, 16
+//   heads of width 128 on 4. Their sum, in M and below the fraction, is of fp32 weights in both.
 // * Where the tiles leave CUs idle the histories are split into slices whose terminal
 //   states a second kernel merges, as the paged decode step does.
 // * The requests' tokens are packed; where they start is device data. Every
@@ -306,14 +314,15 @@ __device__ __forceinline__ void slow_keys64(const unsigned char* Ks, const unsig
                                             int pos, const typename P::Op (&qop)[D / 16], floatx16 (&oacc)[D / 32],
                                             float& m, float& l, float& uii, const Lane& L, int lane, float c) {
   constexpr int KS = D / 16;
+  constexpr bool kParts = sizeof(typename P::T) == 2;  // as the first scan of few rows; it is rare enough for all to have them
   for (int b = 0; b < 2; ++b) {
     const int k0 = kglob + 32 * b;
     if (k0 > phi) break;
     const floatx16 s = evidence<P, KS>(Ks, 32 * b, qop, L);
     if (k0 + 31 < plo) {
-      scan_block<P, D, QM, false>(s, oacc, m, l, uii, Vs, 2 * b, L, 0, c);
+      scan_block<P, D, QM, false, false, kParts>(s, oacc, m, l, uii, Vs, 2 * b, L, 0, c);
     } else {
-      scan_block<P, D, QM, true, true>(s, oacc, m, l, uii, Vs, 2 * b, L, pos - k0, c);
+      scan_block<P, D, QM, true, true, kParts>(s, oacc, m, l, uii, Vs, 2 * b, L, pos - k0, c);
       add_not_finite<P, D>(Vs, 32 * b, pos - k0, oacc, L, lane);
     }
   }
@@ -445,6 +454,7 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
   constexpr int QM = sizeof(E) == 4 ? 1 : 0;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = kBK * P::ROWB;
+  constexpr bool kParts = sizeof(E) == 2;  // weights of few rows are in two parts
   // separate objects: the compiler can then see that reads of one do not wait for the loads in flight into another
   __shared__ __attribute__((aligned(1024))) unsigned char KA[TB];
   __shared__ __attribute__((aligned(1024))) unsigned char VA[TB];
@@ -535,8 +545,14 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
       asm volatile("" ::: "memory");  // no read of them before
       Op pop[2];
       const floatx16 s = evidence<P, KS>(Ks, krow, qop, L);
-      fast_block<P, D, QM, true>(s, m, l, uii, pop, L, me.pos - kt * kBK - krow, c);
-      add_values<P, D>(Vs, krow, 0, pop, oacc, L);
+      if constexpr (kParts) {
+        Op rest[2];
+        fast_block<P, D, QM, true, true>(s, m, l, uii, pop, L, me.pos - kt * kBK - krow, c, rest);
+        add_values<P, D>(Vs, krow, 0, pop, rest, oacc, L);
+      } else {
+        fast_block<P, D, QM, true>(s, m, l, uii, pop, L, me.pos - kt * kBK - krow, c);
+        add_values<P, D>(Vs, krow, 0, pop, oacc, L);
+      }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads from LDS have ended
     }

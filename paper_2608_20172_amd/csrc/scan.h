@@ -66,11 +66,26 @@ __device__ __forceinline__ floatx8 finite_part(floatx8 x) {
   return x;
 }
 
+// What the rounding of the weights p to the operand hi leaves of them, as an operand: bf16 weights of two parts
+// have 16 significant bits.
+template <class P>
+__device__ __forceinline__ typename P::Op rest_of(const float (&p)[8], const typename P::Op& hi) {
+  static_assert(sizeof(typename P::T) == 2, "fp32 weights have no rest");
+  const uintx4 u = __builtin_bit_cast(uintx4, hi);
+  float r[8];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    r[2 * t] = p[2 * t] - bf16_lo(u[t]);
+    r[2 * t + 1] = p[2 * t + 1] - bf16_hi(u[t]);
+  }
+  return P::pack(r);
+}
+
 // One 32-key block of the scan for this wave's 32 rows: s holds the block's
 // evidence (layout of a 32x32 accumulator, keys on rows, queries on lanes);
 // Vs is the V tile and vslice the index of the block's first 16-key slice. CLEAN:
-// values that are not finite count as 0.
-template <class P, int D, int QM, bool DIAG, bool CLEAN = false>
+// values that are not finite count as 0. TWO: bf16 weights in two parts.
+template <class P, int D, int QM, bool DIAG, bool CLEAN = false, bool TWO = false>
 __device__ __forceinline__ void scan_block(floatx16 s, floatx16 (&oacc)[D / 32], float& m, float& l,
                                            float& uii, const unsigned char* Vs, int vslice,
                                            const Lane& L, int self, float c) {
@@ -102,11 +117,14 @@ __device__ __forceinline__ void scan_block(floatx16 s, floatx16 (&oacc)[D / 32],
       l += p[t];
     }
     const Op pop = P::pack(p);
+    Op rest;
+    if constexpr (TWO) rest = rest_of<P>(p, pop);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       Op vop = P::col_op(Vs, vslice + hh, 32 * db, L);
       if (CLEAN) vop = finite_part(vop);
       oacc[db] = P::mma(vop, pop, oacc[db]);
+      if constexpr (TWO) oacc[db] = P::mma(vop, rest, oacc[db]);
     }
   }
 }
@@ -128,10 +146,11 @@ __device__ __forceinline__ floatx16 evidence(const unsigned char* Ks, int krow0,
 }
 
 // A block of the scan with the reference m held fixed: the logits of the block,
-// the packed weights P of its two 16-key halves and their sum into l.
-template <class P, int D, int QM, bool DIAG>
+// the packed weights P of its two 16-key halves and their sum into l; with TWO
+// the rest of the bf16 weights as well.
+template <class P, int D, int QM, bool DIAG, bool TWO = false>
 __device__ __forceinline__ void fast_block(floatx16 s, float m, float& l, float& uii, typename P::Op (&pop)[2],
-                                           const Lane& L, int self, float c) {
+                                           const Lane& L, int self, float c, typename P::Op* rest = nullptr) {
   if (DIAG && holds_self(self, L.g)) uii = pick(s, row_reg(self));
   float mx = kNegInf;
   exchange_logits<DIAG, QM, false>(s, L, self, c, m, mx);
@@ -146,6 +165,7 @@ __device__ __forceinline__ void fast_block(floatx16 s, float m, float& l, float&
       l += p[t];
     }
     pop[hh] = P::pack(p);
+    if constexpr (TWO) rest[hh] = rest_of<P>(p, pop[hh]);
   }
 }
 
@@ -158,6 +178,19 @@ __device__ __forceinline__ void add_values(const unsigned char* Vs, int krow0, i
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
       oacc[db] = P::mma(P::col_op(Vs, krow0 / 16 + 2 * b + hh, 32 * db, L), pop[hh], oacc[db]);
+}
+// The same of weights in two parts.
+template <class P, int D>
+__device__ __forceinline__ void add_values(const unsigned char* Vs, int krow0, int b, const typename P::Op (&pop)[2],
+                                           const typename P::Op (&rest)[2], floatx16 (&oacc)[D / 32], const Lane& L) {
+#pragma unroll
+  for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const typename P::Op vop = P::col_op(Vs, krow0 / 16 + 2 * b + hh, 32 * db, L);
+      oacc[db] = P::mma(vop, pop[hh], oacc[db]);
+      oacc[db] = P::mma(vop, rest[hh], oacc[db]);
+    }
 }
 
 // The 64 keys krow0 .. krow0+63 of a tile, all before every row of the wave, with the reference held fixed.

@@ -426,3 +426,33 @@ def test_prefill_sizes_between_few_and_many_tiles(B, H, D, n, dtype):
     chunks = [((b * 131) % 400, max(1, n - 17 * b)) for b in range(B)]
     s = _step(chunks, H, 1, D, 16, dtype)
     _close(_run(s), s, dtype, most=24)
+
+
+@pytest.mark.parametrize("chunks,H,G,D", [
+    ([(200, 1), (40, 1), (700, 1)], 2, 1, 64), ([(1000, 1)] * 20, 4, 4, 128), ([(333, 20)], 8, 1, 64), ([(5000, 3)], 2, 2, 96),
+    ([(2000, 1)] * 8 + [(100, 130)] * 4, 4, 4, 128), ([(9000, 1)], 1, 32, 80),
+])
+@pytest.mark.parametrize("again", [False, True])
+def test_prefill_weights_of_few_rows_are_as_the_decode_steps(chunks, H, G, D, again):
+    """Where a request has at most 32 rows of a key head, its weights are as exact as the decode step's: with all
+    values 1 the row is their sum over itself, 1 to 2^-16 for weights of 16 significant bits, so 1 in bf16; with equal keys the
+    rounding of a weight to 8 bits would stand there whole. again: totals over 2^62, which are summed a second time."""
+    rng = np.random.default_rng(len(chunks))
+    s = _step(chunks, H, G, D, 16, "bf16")
+    s["vc"].fill_(1.0)
+    s["kc"].fill_(0.25)
+    # U = scale sum(q) / 4, another for every row, from 2 on; or from 60
+    N = int(s["start"][-1])
+    u = torch.from_numpy(rng.random((N, H * G, 1)) * 6 + (60 if again else 2)).to(DEV)
+    s["q"] = (u * 4 / math.sqrt(D) * torch.ones(D, device=DEV)).to(torch.bfloat16)
+    r = _run(s)
+    for b, (c, n) in enumerate(chunks):
+        if n * G > 32:
+            continue
+        at = slice(int(s["start"][b]), int(s["start"][b + 1]))
+        assert bool((r["o"][at] == 1).all()), (b, float((r["o"][at].float() - 1).abs().max()))
+    one = [b for b, (c, n) in enumerate(chunks) if n == 1]
+    if one:
+        at = torch.tensor([int(s["start"][b]) for b in one], device=DEV)
+        d = R.relation_paged_decode(s["q"][at], s["kc"], s["vc"], _i32(s["table"][one]), _i32(s["lens"][one]), 0.4)
+        assert bool((d["o"] == 1).all())
