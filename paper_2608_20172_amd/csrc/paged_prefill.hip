@@ -588,7 +588,8 @@ __global__ __launch_bounds__(kNT, (prefill_occupancy<P, D>())) void prefill_kern
   }
   if (bad != kNone) atomicMin(&bad_key, bad);
   // As in the fused forward pass the scan ran with the reference at 0, which is exact while the row total stays under
-  // 2^64 (2^62 in each of four waves). Sums that are not finite come from values that are not, perhaps behind the row.
+  // 2^64; 2^62 is asked for here, in every tile, so that the four parts of one of few rows stay under it together. Sums
+  // that are not finite come from values that are not, perhaps behind the row.
   const float lt = l + xor32(l);
   float f = 0.0f;
 #pragma unroll
