@@ -550,7 +550,9 @@ rel_status relation_paged_decode(const rel_pages* c, const rel_paged_query* d, c
  *   workspace  relation_paged_prefill_workspace_bytes(c, d) bytes, 16-byte aligned.
  *              Fewer tokens may need more (their histories are split further): what
  *              calls of several sizes share is the largest of theirs
- * max_length as in rel_paged_query. A request whose length is under n_b or over
+ * max_length as in rel_paged_query; the rows of a tile and the slices of the histories
+ * go by it, so that a table much wider than the requests wants it given (one prompt of
+ * 2048 tokens, 8 heads x 64, in a table of 32768: 49 us without, 26 with). A request whose length is under n_b or over
  * that bound gets NaN rows, and so does a row if a page of its entries is not in the
  * pool. Entries past a request's length are not read; NaN and infinities in the
  * entries after a row do not reach it. An infinite value among a row's own entries

@@ -888,7 +888,8 @@ def relation_paged_prefill(q, k_cache, v_cache, table, lengths, row_start, lam, 
     """A chunk of new tokens of each request over pages: q [N, Hq, D], request b's tokens in rows row_start[b] ..
     row_start[b + 1] - 1 (int32 [B + 1], as relation_page_map gives it), which are its last ones: positions up to
     lengths[b] (int32 [B]), their keys and values in the caches [num_pages, H, page_size, D] already. table int32
-    [B, W]; max_length, scale, head_dim as for relation_paged_decode. Returns dict(o [N, Hq, D], row_stat [N, Hq]).
+    [B, W]; max_length, scale, head_dim as for relation_paged_decode; how the step is cut goes by max_length too, so give it
+    where the table is much wider than the requests. Returns dict(o [N, Hq, D], row_stat [N, Hq]).
     Rows of no request are not written: give ``out`` where they have to hold something."""
     lib = load_library()
     dev = _on_gpu(q, k_cache, v_cache, table, lengths, row_start)

@@ -730,10 +730,11 @@ hipError_t launch_one(PagedPrefillArgs a, hipStream_t stream) {
 // Rows of a tile and slices of the histories, by sizes alone (the lengths are device data), so that the chip is full.
 // * Tiles of 32 rows where tiles of 128 would not give every CU one and the histories are short, and, where requests
 //   have 64 rows and more, up to two tiles a CU of 64 channels, five for four CUs of more. One prompt of 2048 tokens, 8
-//   heads x 64, 26 us against 42, four 45 against 59 (416 tiles), two of 4096 68 against 87 (400); 8 heads x 128, one of
-//   4096 88 against 101 (264), but four of 2048 84 against 74 (416); five chunks of 151 to 301 tokens after up to 777, 8
-//   heads x 80 in fp32, 88 against 327. With longer histories the keys that every tile reads again cost more than
-//   slices of 128-row tiles: a chunk of 64 tokens after 16384, 8 heads x 64, takes 29 us in 32 slices, 274 in one.
+//   heads x 64, 27 us against 33 in slices of 128-row tiles, four of 1536 39 against 46 (416 tiles), two of 3000 60 against
+//   63 (384); 8 heads x 128, one of 4096 93 against 95 (264), but four of 1536 71 against 61 (416); five chunks of 151 to 301
+//   tokens after up to 777, 8 heads x 80 in fp32, 87 against 109. With longer histories the keys that every tile reads
+//   again cost more than slices of 128-row tiles: a chunk of 64 tokens after 16384, 8 heads x 64, takes 31 us in 32 slices,
+//   274 in one.
 // * As many slices as bring the workgroups to what the chip holds at once (three a CU for bf16 of up to 64 channels,
 //   else two), each of 512 keys or more: a chunk of 2048 after 32768, 16 heads on 4 x 128, 687 to 716 us in two slices,
 //   903 to 927 in one, 683 to 706 in four; 7 chunks of 128 to 256 after up to 4096 78 in four, 124 in one. Tiles of 32

@@ -456,3 +456,20 @@ def test_prefill_weights_of_few_rows_are_as_the_decode_steps(chunks, H, G, D, ag
         at = torch.tensor([int(s["start"][b]) for b in one], device=DEV)
         d = R.relation_paged_decode(s["q"][at], s["kc"], s["vc"], _i32(s["table"][one]), _i32(s["lens"][one]), 0.4)
         assert bool((d["o"] == 1).all())
+
+
+@pytest.mark.parametrize("chunks,H,G,D,dtype", [
+    ([(201, 24)], 8, 1, 64, "bf16"), ([(0, 300), (500, 1), (0, 1), (70, 3)], 2, 4, 128, "bf16"), ([(0, 700)], 2, 1, 64, "bf16"),
+    ([(100, 60), (9, 0), (0, 33)], 2, 2, 80, "f32"),
+])
+def test_prefill_table_wider_than_the_requests(chunks, H, G, D, dtype):
+    """A table of 32768 tokens a request, as a serving loop keeps for its longest context: tiles and slices go by it, most
+    slices have no keys. With max_length and without, against the oracle."""
+    s = _step(chunks, H, G, D, 16, dtype)
+    wide = np.full((len(chunks), 2048), -1)
+    wide[:, :s["table"].shape[1]] = s["table"]
+    s["table"] = wide
+    for kw in ({}, {"max_length": int(max(s["lens"]))}, {"max_length": 5000}):
+        r = _run(s, **kw)
+        _close(r, s, dtype)
+        assert not torch.isnan(r["o"]).any()
