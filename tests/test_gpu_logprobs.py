@@ -339,7 +339,7 @@ def test_given_outputs_and_arguments():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V,left", [(260, 4), (261, 5), (263, 7), (300, 3), (515, 3), (516, 4), (517, 1), (772, 4), (2050, 2),
-                                    (4099, 3), (30725, 5), (61445, 5)])
+                                    (4099, 3), (30981, 5), (61445, 5)])
 def test_rows_masked_everywhere_but_at_the_end(V, left, dtype):
     """A mask of a finite value under -2^119 on all but the last logits: the alternatives past those are masked tokens, the
     lowest indices first, each once."""
@@ -355,7 +355,7 @@ def test_rows_masked_everywhere_but_at_the_end(V, left, dtype):
     _check(x, [0, V - left, 1, V - 2, 3, V // 2], 20)
 
 
-@pytest.mark.parametrize("dtype,V", [("f32", 30725), ("f32", 31743), ("bf16", 61445), ("bf16", 63487)])
+@pytest.mark.parametrize("dtype,V", [("f32", 30981), ("f32", 31743), ("bf16", 61445), ("bf16", 63487)])
 def test_many_rows_masked_everywhere_but_at_the_end(V, dtype):
     """The same in a workgroup's last of several sub-chunks, when all before it are masked."""
     N, left = 600, V % 1024 if V % 1024 < 8 else 5
