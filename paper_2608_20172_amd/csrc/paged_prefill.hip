@@ -38,9 +38,11 @@
 // What bounds it is the vector work of a weight, about 9 instructions a lane and
 // entry beside one matrix instruction, as in the fused forward pass, and the waits
 // of a gather: a chunk of 2048 tokens after 32768, 16 heads of width 128 on 4, takes
-// 665 to 693 us (0.82 PFLOP/s and more), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
+// 660 to 690 us (0.82 PFLOP/s and more), 8 prompts of 1024 to 2048 tokens, 12 heads x 64, 73 us. On
 // the same rows in one dense tensor the fused forward pass, which looks nothing up,
-// takes 62 us against 71 (8 x 12 x 1536 x 64) and 167 against 194 (4 x 8 x 4096 x 128).
+// takes 55 us against 61 (8 x 12 x 1536 x 64) and 164 against 185 (4 x 8 x 4096 x 128). In
+// fp32 over 64 channels it is the LDS: the 32 rows of K that a half-wave reads stand 512
+// bytes apart, on one bank (92% of the LDS's busy cycles at D = 80 are conflicts).
 #include "kernels.h"
 #include "lanes.h"
 #include "paged_row.h"
